@@ -11,7 +11,7 @@
  *   - The caller owns every buffer.  The library never allocates, frees or
  *     synchronises; all work is enqueued on `cuda_stream` (a cudaStream_t passed as
  *     void*, NULL = the legacy default stream) and returns immediately.
- *   - Inputs are never modified.  Outputs are overwritten (never accumulated into).
+ *   - Inputs are never modified.  Outputs are overwritten (never accumulated into; where a call works in place or accumulates, it says so).
  *     No output may alias an input or another output.
  *   - All tensors of one call share `dtype`; products are accumulated in fp32 and
  *     rounded once (round-to-nearest-even) to `dtype` at the final store.  With
@@ -337,6 +337,133 @@ int pf_pack_factor_grads(const void* const* grads, const int64_t* numels, int co
 int pf_unpack_factor_grads(const void* flat, int64_t flat_elems, void* const* grads, const int64_t* numels,
                            int count, int dtype, int64_t* offsets_out,
                            void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* ---------------------------------------------------------------------------------
+ * Tokens of a layer with experts, for the grouped layers above: [experts, capacity, k] is the grouped forward's x with one
+ * factor pair per expert.  `tokens` tokens choose `k` of `experts` experts each; assignment a = token * k + j goes to
+ * expert ids[a].  (The paper has no counterpart; a factorized feed-forward layer is the expert.)
+ *
+ * pf_expert_sort gives every assignment a row.  An expert's assignments keep their order; the r-th of expert e gets row
+ *   capacity > 0:  e * capacity + r, none from r = capacity on;      rows = experts * capacity
+ *   capacity = 0:  offsets[e] + r, expert after expert without gaps;  rows = tokens * k
+ * An id outside 0 .. experts - 1 gets no row.  The same expert may be chosen twice by a token (two rows).
+ *   ids     [tokens, k]   int32
+ *   slots   [tokens, k]   int32  row of each assignment, -1 for none
+ *   sources [rows]        int32  assignment of each row, -1 for none
+ *   counts  [experts]     int32  assignments that chose the expert, those without a row among them
+ *   offsets [experts + 1] int32  first row of each expert; behind the last, experts * capacity or the rows in use
+ * One launch of up to eight blocks, no workspace.  PF_ERR_UNSUPPORTED: more than 2048 experts, or 2^30 assignments or rows.
+ * pf_expert_rows returns `rows` (0 for invalid sizes).
+ *
+ * The other four take slots and sources as pf_expert_sort left them (an index outside the rows counts as none) and
+ * matrices of `width` columns at any pitch; x, y, dx, dy have `tokens` rows, xs, ys, dxs, dys `rows`:
+ *   dispatch_fwd   xs[slots[t, j]] = x[t]; rows without an assignment are zeroed
+ *   dispatch_bwd   dx[t]  = sum over j of dxs[slots[t, j]]
+ *   combine_fwd    y[t]   = sum over j of weights[t, j] ys[slots[t, j]]                weights [tokens, k] fp32, NULL = ones
+ *   combine_bwd    dys[slots[t, j]] = weights[t, j] dy[t], other rows zeroed;  dweights[t, j] = <dy[t], ys[slots[t, j]]>, 0 without a row
+ *                  (dys or dweights may be NULL: not wanted)
+ * Sums run over j in order, in fp32, and are rounded once; assignments without a row add nothing, so a token all of whose
+ * assignments were dropped gives zeros.  dweights is fp32.  What rows without an assignment hold is never read.  One launch each, no workspace.
+ * ------------------------------------------------------------------------------- */
+int64_t pf_expert_rows(int64_t tokens, int k, int experts, int64_t capacity);
+
+int pf_expert_sort(const int32_t* ids, int64_t tokens, int k, int experts, int64_t capacity,
+                   int32_t* slots, int32_t* sources, int32_t* counts, int32_t* offsets, void* cuda_stream);
+
+int pf_expert_dispatch_fwd(const void* x, int64_t ldx, const int32_t* slots, const int32_t* sources, void* xs, int64_t ldxs,
+                           int64_t tokens, int k, int64_t rows, int64_t width, int dtype, void* cuda_stream);
+
+int pf_expert_dispatch_bwd(const void* dxs, int64_t lddxs, const int32_t* slots, void* dx, int64_t lddx,
+                           int64_t tokens, int k, int64_t rows, int64_t width, int dtype, void* cuda_stream);
+
+int pf_expert_combine_fwd(const void* ys, int64_t ldys, const int32_t* slots, const float* weights, void* y, int64_t ldy,
+                          int64_t tokens, int k, int64_t rows, int64_t width, int dtype, void* cuda_stream);
+
+int pf_expert_combine_bwd(const void* ys, int64_t ldys, const int32_t* slots, const int32_t* sources, const float* weights,
+                          const void* dy, int64_t lddy, void* dys, int64_t lddys, float* dweights,
+                          int64_t tokens, int k, int64_t rows, int64_t width, int dtype, void* cuda_stream);
+
+/* ---------------------------------------------------------------------------------
+ * Norm and position rotation of queries and keys, for each head: what follows the projections W^Q and W^K of an attention
+ * layer (Section 2.4; grouped layers above) where its heads are normalised and its positions are rotations.  For a row x of
+ * `dim` elements (one head of the token at position t):
+ *   z = x / sqrt(mean(x^2) + eps) * w,   then the first rot_dim elements of z are pairs (a, b), pair i turned by t * inv_freq[i]:
+ *   (a, b) -> (a cos - b sin, b cos + a sin)
+ * PF_ROPE_HALVES pairs element i with rot_dim / 2 + i, PF_ROPE_PAIRS element 2 i with 2 i + 1; the other elements stay as they are.
+ *   q, q_out [tokens, q_heads, dim]: token t's head h starts at t * ldq + h * sq ELEMENTS; k, k_out likewise (k_heads).  Any
+ *            strides under which rows do not overlap (heads inside tokens or tokens inside heads); elements of a row are contiguous.
+ *   wq, wk   [dim] in `dtype`, NULL = ones        inv_freq [rot_dim / 2] fp32        positions [tokens] int64, NULL = 0, 1, 2, ...
+ * Statistics and products are in fp32 and rounded once; an angle is reduced to a part of a turn before it is
+ * rounded to fp32, so that far positions (up to 2^53) keep it.  Either of q_heads and k_heads may be 0 (its pointers are ignored then).  rot_dim is even,
+ * 0 .. dim.  PF_ERR_UNSUPPORTED: dim > 1024, more than 65536 heads or 2^31 tokens.  One launch, no workspace.
+ *
+ * Backward, for the gradients dq_out and dk_out of the outputs: dq, dk (in `dtype`; always written), and dwq, dwk [dim] (sums over
+ * tokens and heads in a fixed order, fp32, rounded once; NULL = not wanted).  The norm's statistics are computed again from q and k.
+ * flags: PF_GRAD_ACCUMULATE adds to dwq and dwk (dq and dk are never accumulated), PF_GRAD_F32 makes them fp32.  The workspace is
+ * needed only when dwq or dwk is given, which also takes a second launch.  tokens = 0 zeroes dwq and dwk (accumulating: leaves them).
+ * ------------------------------------------------------------------------------- */
+typedef enum {
+    PF_ROPE_HALVES = 0,
+    PF_ROPE_PAIRS = 1
+} pf_rope_style;
+
+int pf_qk_norm_rope_fwd(const void* q, int64_t ldq, int64_t sq, const void* k, int64_t ldk, int64_t sk,
+                        const void* wq, const void* wk, const int64_t* positions, const float* inv_freq,
+                        void* q_out, int64_t ldqo, int64_t sqo, void* k_out, int64_t ldko, int64_t sko,
+                        int64_t tokens, int q_heads, int k_heads, int dim, int rot_dim, int style, double eps, int dtype,
+                        void* cuda_stream);
+
+size_t pf_qk_norm_rope_bwd_workspace(int64_t tokens, int q_heads, int k_heads, int dim);
+
+int pf_qk_norm_rope_bwd(const void* q, int64_t ldq, int64_t sq, const void* k, int64_t ldk, int64_t sk,
+                        const void* wq, const void* wk, const int64_t* positions, const float* inv_freq,
+                        const void* dq_out, int64_t lddqo, int64_t sdqo, const void* dk_out, int64_t lddko, int64_t sdko,
+                        void* dq, int64_t lddq, int64_t sdq, void* dk, int64_t lddk, int64_t sdk, void* dwq, void* dwk,
+                        int64_t tokens, int q_heads, int k_heads, int dim, int rot_dim, int style, double eps, int dtype,
+                        unsigned flags, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* ---------------------------------------------------------------------------------
+ * AdamW over a list of tensors, IN PLACE: the step behind the exchange of the flat gradient buffer (Section 4.1).  Tensor i of
+ * numels[i] elements, t = step:
+ *   g = grad_scale * grad        m <- beta1 m + (1 - beta1) g        v <- beta2 v + (1 - beta2) g^2
+ *   p <- p - lr (weight_decay p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+ * in fp32, m and v with each product and sum rounded by itself.
+ *   params   in param_dtype.  masters: NULL, or (PF_BF16 parameters) fp32 masters, which are then what is read and stepped;
+ *            params receives them rounded.  Without masters a PF_BF16 parameter is stepped in fp32 and rounded once.
+ *   grads    in grad_dtype, read only: the slices of a flat buffer as they are (element alignment) or any other tensors
+ *   state    PF_STATE_F32: m, v fp32.
+ *            PF_STATE_8BIT: m is 8-bit floats of the e4m3 format, v of the e5m2 format, each times the fp32 scale of its block of 256
+ *            elements (counted from the tensor's first): m_scales, v_scales [ceil(numels[i] / 256)].  Zeroed codes and scales are
+ *            the state before the first step.  Scales are powers of two that put the largest of a block into [128, 256) (m) and [2^14, 2^15) (v).
+ *            A value is rounded up with the probability of what is cut off (16 bits of a hash of seed, i and the element's place in its
+ *            tensor; give each step another seed): rounding to nearest would leave v as it is once 1 - beta2 is
+ *            below half a step of the format.  Under the format's smallest normal number m becomes 0 and v > 0 that number; what is not
+ *            finite becomes NaN.  p is stepped with m and v before they are rounded.
+ * numels, and the lists of pointers, are host arrays of `count`; tensors with numels 0 are skipped (but count as places).  The
+ * arrays of different tensors must not overlap.
+ * scalars: NULL, or a device array (4-byte aligned) that replaces lr, step (by the two corrections), grad_scale and seed, for
+ * steps replayed from a CUDA graph.  The library reads it when the step runs.
+ * One launch for up to 256 tensors, no workspace. */
+typedef enum {
+    PF_STATE_F32 = 0,
+    PF_STATE_8BIT = 1
+} pf_state;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay; /* finite; 0 <= beta < 1, eps >= 0 */
+    int64_t step;                               /* t >= 1: 1 for the first step */
+    float grad_scale;                           /* 1 = none; the inverse of a loss scale, a clipping factor */
+    uint32_t seed;                              /* of the rounding of 8-bit states */
+} pf_adamw;
+typedef struct {
+    float lr;
+    float correction1, correction2; /* 1 - beta1^t, 1 - beta2^t */
+    float grad_scale;
+    uint32_t seed;
+} pf_adamw_scalars;
+int pf_adamw_step(void* const* params, float* const* masters, const void* const* grads, void* const* m, void* const* v,
+                  float* const* m_scales, float* const* v_scales, const int64_t* numels, int count,
+                  int param_dtype, int grad_dtype, int state, const pf_adamw* hyper, const pf_adamw_scalars* scalars,
+                  void* cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -17,6 +17,8 @@ import torch
 PF_F32, PF_BF16 = 0, 1
 PF_ACT_NONE, PF_ACT_RELU = 0, 1
 PF_GRAD_ACCUMULATE, PF_GRAD_F32 = 1, 2
+PF_ROPE_HALVES, PF_ROPE_PAIRS = 0, 1
+PF_STATE_F32, PF_STATE_8BIT = 0, 1
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libpf.so")
 _lib = None
@@ -85,6 +87,28 @@ def lib() -> ctypes.CDLL:
         L.pf_pack_factor_grads.argtypes = [vp, vp, ci, ci, vp, i64, vp, vp, sz, vp]
         L.pf_unpack_factor_grads.restype = ci
         L.pf_unpack_factor_grads.argtypes = [vp, i64, vp, vp, ci, ci, vp, vp, sz, vp]
+        L.pf_expert_rows.restype = i64
+        L.pf_expert_rows.argtypes = [i64, ci, ci, i64]
+        L.pf_expert_sort.restype = ci
+        L.pf_expert_sort.argtypes = [vp, i64, ci, ci, i64, vp, vp, vp, vp, vp]
+        sizes = [i64, ci, i64, i64, ci, vp]
+        L.pf_expert_dispatch_fwd.restype = ci
+        L.pf_expert_dispatch_fwd.argtypes = [vp, i64, vp, vp, vp, i64] + sizes
+        L.pf_expert_dispatch_bwd.restype = ci
+        L.pf_expert_dispatch_bwd.argtypes = [vp, i64, vp, vp, i64] + sizes
+        L.pf_expert_combine_fwd.restype = ci
+        L.pf_expert_combine_fwd.argtypes = [vp, i64, vp, vp, vp, i64] + sizes
+        L.pf_expert_combine_bwd.restype = ci
+        L.pf_expert_combine_bwd.argtypes = [vp, i64, vp, vp, vp, vp, i64, vp, i64, vp] + sizes
+        heads = [i64, ci, ci, ci, ci, ci, ctypes.c_double, ci]
+        L.pf_qk_norm_rope_fwd.restype = ci
+        L.pf_qk_norm_rope_fwd.argtypes = [vp, i64, i64] * 2 + [vp] * 4 + [vp, i64, i64] * 2 + heads + [vp]
+        L.pf_qk_norm_rope_bwd_workspace.restype = sz
+        L.pf_qk_norm_rope_bwd_workspace.argtypes = [i64, ci, ci, ci]
+        L.pf_qk_norm_rope_bwd.restype = ci
+        L.pf_qk_norm_rope_bwd.argtypes = [vp, i64, i64] * 2 + [vp] * 4 + [vp, i64, i64] * 4 + [vp, vp] + heads + [ctypes.c_uint, vp, sz, vp]
+        L.pf_adamw_step.restype = ci
+        L.pf_adamw_step.argtypes = [vp] * 8 + [ci] * 4 + [vp] * 3
         _lib = L
     return _lib
 
@@ -230,3 +254,83 @@ def pf_unpack_factor_grads(flat, grads, *, stream=None):
         return [0]
     n = _native or _load_native()
     return n.unpack(flat, grads, stream)
+
+
+def pf_expert_rows(tokens, k, experts, capacity=0) -> int:
+    return int(lib().pf_expert_rows(tokens, k, experts, capacity))
+
+
+def pf_expert_sort(ids, experts, *, capacity=0, slots=None, sources=None, counts=None, offsets=None, stream=None, prepare=False):
+    """Rows of a layer's experts for the assignments ids [tokens, k] (int32).  Returns (slots [tokens, k], sources [rows],
+    counts [experts], offsets [experts + 1]), all int32; rows = experts * capacity, or tokens * k without a capacity."""
+    n = _native or _load_native()
+    return n.expert_sort(ids, experts, capacity, slots, sources, counts, offsets, stream, prepare)
+
+
+def pf_expert_dispatch_fwd(x, slots, sources, *, xs=None, stream=None, prepare=False):
+    """Tokens' rows x [tokens, width] in their experts' rows xs [rows, width] (rows without a token are zero); with a capacity
+    xs.view(experts, capacity, width) is what pf_lowrank_linear_grouped_fwd takes."""
+    n = _native or _load_native()
+    return n.expert_dispatch_fwd(x, slots, sources, xs, stream, prepare)
+
+
+def pf_expert_dispatch_bwd(dxs, slots, *, dx=None, stream=None, prepare=False):
+    """dx [tokens, width]: for each token the sum of its experts' rows of dxs [rows, width]."""
+    n = _native or _load_native()
+    return n.expert_combine_fwd(dxs, slots, None, dx, stream, prepare, True)
+
+
+def pf_expert_combine_fwd(ys, slots, weights=None, *, y=None, stream=None, prepare=False):
+    """y [tokens, width]: for each token the sum of its experts' rows of ys [rows, width] times weights [tokens, k] (float32)."""
+    n = _native or _load_native()
+    return n.expert_combine_fwd(ys, slots, weights, y, stream, prepare, False)
+
+
+def pf_expert_combine_bwd(ys, slots, sources, weights, dy, *, need_dys=True, dys=None, need_dweights=True, dweights=None, stream=None,
+                          prepare=False):
+    """Returns (dys [rows, width] or None, dweights [tokens, k] float32 or None) for the upstream gradient dy [tokens, width]."""
+    n = _native or _load_native()
+    return n.expert_combine_bwd(ys, slots, sources, weights, dy, need_dys, dys, need_dweights, dweights, stream, prepare)
+
+
+def pf_qk_norm_rope_fwd(q, k, wq, wk, inv_freq, *, positions=None, style=PF_ROPE_HALVES, eps=1e-6, q_out=None, k_out=None, stream=None,
+                        prepare=False):
+    """Root-mean-square norm of each head of q [tokens, q_heads, dim] and k [tokens, k_heads, dim] (either may be None; any strides of
+    tokens and heads), times wq, wk [dim] or None, its first 2 * len(inv_freq) elements rotated by positions [tokens] (int64;
+    None: 0, 1, ...) times inv_freq (float32).  Returns (q_out, k_out)."""
+    n = _native or _load_native()
+    return n.qk_fwd(q, k, wq, wk, inv_freq, positions, style, eps, q_out, k_out, stream, prepare)
+
+
+def pf_qk_norm_rope_bwd_workspace(tokens, q_heads, k_heads, dim) -> int:
+    return int(lib().pf_qk_norm_rope_bwd_workspace(tokens, q_heads, k_heads, dim))
+
+
+def pf_qk_norm_rope_bwd(q, k, wq, wk, inv_freq, dq_out, dk_out, *, positions=None, style=PF_ROPE_HALVES, eps=1e-6, dq=None, dk=None,
+                        need_dw=True, dwq=None, dwk=None, accumulate=False, grads_f32=False, workspace=None, stream=None, prepare=False):
+    """Returns (dq, dk, dwq, dwk) for the gradients of pf_qk_norm_rope_fwd's outputs; dwq and dwk are None where there is no weight
+    or need_dw=False.  accumulate: dwq and dwk (required then) are added to; grads_f32: they are float32."""
+    n = _native or _load_native()
+    return n.qk_bwd(q, k, wq, wk, inv_freq, positions, style, eps, dq_out, dk_out, dq, dk, need_dw, dwq, dwk, accumulate, grads_f32,
+                    workspace, stream, prepare)
+
+
+def pf_adamw_scalars(*, lr, betas=(0.9, 0.999), step, grad_scale=1.0, seed=0):
+    """The five values that replace lr, step, grad_scale and seed of a pf_adamw_step with scalars=: a float32 tensor on the host
+    (the seed's bits in the last), to be copied into the device tensor that the step reads."""
+    t = torch.tensor([lr, 1 - betas[0] ** step, 1 - betas[1] ** step, grad_scale, 0], dtype=torch.float32)
+    t.view(torch.int32)[4] = seed - (1 << 32) if seed >= 1 << 31 else seed
+    return t
+
+
+def pf_adamw_step(params, grads, m, v, *, masters=None, m_scales=None, v_scales=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8,
+                  weight_decay=0.01, step=1, grad_scale=1.0, seed=0, scalars=None, stream=None, prepare=False):
+    """One AdamW step in place over lists of contiguous CUDA tensors.  m and v are float32, or float8_e4m3fn and float8_e5m2 with
+    m_scales and v_scales (float32, one for each 256 elements of a tensor); masters (float32) go with bfloat16 parameters.
+    scalars: a float32 CUDA tensor with the values of pf_adamw_scalars, read when the step runs.  Returns None
+    (prepare=True: (call, None))."""
+    if len(params) == 0:
+        return ((lambda: None), None) if prepare else None
+    n = _native or _load_native()
+    return n.adamw_step(params, grads, m, v, masters, m_scales, v_scales, lr, betas[0], betas[1], eps, weight_decay, step, grad_scale, seed,
+                        scalars, stream, prepare)

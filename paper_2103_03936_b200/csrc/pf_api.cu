@@ -19,24 +19,6 @@ struct PerDevice {
 };
 PerDevice g_dev[64];
 
-bool elem_aligned(const void* p, int dtype) {
-    return (reinterpret_cast<uintptr_t>(p) % dtype_size(dtype)) == 0;
-}
-bool valid_dtype(int dtype) { return dtype == PF_F32 || dtype == PF_BF16; }
-
-int check_ws(const void* ws, size_t have, size_t need) {
-    if (need == 0) return PF_OK;
-    if (ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || have < need)
-        return PF_ERR_WORKSPACE;
-    return PF_OK;
-}
-
-#define PF_CUDA(expr)                                   \
-    do {                                                \
-        cudaError_t e__ = (expr);                       \
-        if (e__ != cudaSuccess) return PF_ERR_CUDA;     \
-    } while (0)
-
 MatA plainA(const void* p, int64_t s_row, int64_t s_col) {
     MatA a;
     std::memset(&a, 0, sizeof(a));

@@ -30,6 +30,21 @@ inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t dtype_size(int dtype) { return dtype == PF_BF16 ? 2 : 4; }
 
+// Checks of arguments that the entry points share.
+inline bool elem_aligned(const void* p, int dtype) { return (reinterpret_cast<uintptr_t>(p) % dtype_size(dtype)) == 0; }
+inline bool valid_dtype(int dtype) { return dtype == PF_F32 || dtype == PF_BF16; }
+inline int check_ws(const void* ws, size_t have, size_t need) {
+    if (need == 0) return PF_OK;
+    if (ws == nullptr || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || have < need) return PF_ERR_WORKSPACE;
+    return PF_OK;
+}
+
+#define PF_CUDA(expr)                                   \
+    do {                                                \
+        cudaError_t e__ = (expr);                       \
+        if (e__ != cudaSuccess) return PF_ERR_CUDA;     \
+    } while (0)
+
 // ---------------------------------------------------------------------------------------
 // Generic strided / implicit matrix views consumed by the FMA (SIMT) GEMM.  The FMA path
 // serves every shape and layout outside the tensor-core envelopes.
@@ -152,6 +167,28 @@ int linear_fwd_impl(const void* x, int64_t ldx, const void* U, int64_t ldu, cons
 
 // host-side count of kernels launched by this library
 void count_launch(int n = 1);
+
+// A launch that may start beside the tail of the one before in its stream: its kernel executes griddepcontrol.wait before it touches
+// global memory.  cluster > 1: blocks of a cluster, along x.
+template <typename... P, typename... A>
+cudaError_t launch_beside(void (*kernel)(P...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t stream, const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<const P&>(args)...);
+    if (e == cudaSuccess) count_launch();
+    return e;
+}
 
 // device status word (bounded waits report here)
 cudaError_t read_and_clear_device_status(unsigned int* out);

@@ -14,6 +14,7 @@
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDACachingAllocator.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -566,6 +567,369 @@ PyObject* unpack(PyObject* const* a) {
     return offset_list(l.offsets);
 }
 
+// ---------------------------------------------------------------------------- operators around the layers
+// The device of a call's tensors: all of them have to be on one, which is made current for the call.
+struct OnDevice {
+    c10::Device device;
+    c10::cuda::OptionalCUDAGuard guard;
+    explicit OnDevice(const at::Tensor& t, const char* name) : device(t.device()) {
+        if (!t.is_cuda()) value_error(std::string(name) + ": need a CUDA tensor");
+        guard.set_device(device);
+    }
+    // An argument of a dtype and number of dimensions (undefined ones pass).
+    void check(const at::Tensor& t, const char* name, at::ScalarType type, int64_t dims, bool contiguous) const {
+        if (!t.defined()) return;
+        if (t.device() != device || t.scalar_type() != type || t.dim() != dims || (contiguous && !t.is_contiguous()))
+            value_error(std::string(name) + ": need a " + (contiguous ? "contiguous " : "") + c10::toString(type) + " tensor of " + std::to_string(dims) +
+                        " dimensions on " + device.str());
+    }
+};
+// Issues a C call (or prepares it) with the tensors' device current.
+template <typename F>
+PyObject* issue_on(const OnDevice& on, bool prepare, F&& f, const char* where, Workspace&& ws, std::vector<at::Tensor> keep, PyObject* out) {
+    if (!prepare) return issue(false, std::forward<F>(f), where, std::move(ws), {}, out);
+    return issue(true, [f = std::forward<F>(f), index = on.device.index()]() mutable {
+        const c10::cuda::CUDAGuard guard(index);
+        return f();
+    }, where, std::move(ws), std::move(keep), out);
+}
+double real(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw python_error();
+    return v;
+}
+int int_of(PyObject* o, const char* name) {
+    const int64_t v = integer(o);
+    if (v < INT32_MIN || v > INT32_MAX) value_error(std::string(name) + ": out of range");
+    return static_cast<int>(v);
+}
+
+// Rows [tokens, heads, dim] with contiguous elements.
+struct Heads {
+    void* p;
+    int64_t ld, s;
+};
+Heads heads_of(const OnDevice& on, const at::Tensor& t, const char* name, const at::Tensor& like) {
+    if (!t.defined()) return {nullptr, 0, 0};
+    if (!like.defined()) value_error(std::string(name) + ": given without the rows that it goes with");
+    on.check(t, name, like.scalar_type(), 3, false);
+    if (t.sizes() != like.sizes() || (t.size(2) > 1 && t.stride(2) != 1))
+        value_error(std::string(name) + ": need [tokens, heads, dim] with contiguous elements, as q or k");
+    return {t.data_ptr(), t.stride(0), t.stride(1)};
+}
+// What both directions have in common.
+struct Rope {
+    at::Tensor q, k, wq, wk, inv_freq, positions;
+    int64_t tokens;
+    int q_heads, k_heads, dim, rot, dt;
+};
+Rope rope_args(const OnDevice& on, PyObject* const* a) {
+    Rope r{optional(a[0], "q"), optional(a[1], "k"), optional(a[2], "wq"), optional(a[3], "wk"), tensor(a[4], "inv_freq"), optional(a[5], "positions")};
+    const at::Tensor& any = r.q.defined() ? r.q : r.k;
+    r.dt = dtype_code(any);
+    if (any.dim() != 3) value_error("q and k must be [tokens, heads, dim]");
+    if (r.k.defined() && r.q.defined()) {
+        on.check(r.k, "k", r.q.scalar_type(), 3, false);
+        if (r.k.size(0) != r.q.size(0) || r.k.size(2) != r.q.size(2)) value_error("q and k must have the same tokens and dim");
+    }
+    r.tokens = any.size(0);
+    const int64_t dim = any.size(2), q_heads = r.q.defined() ? r.q.size(1) : 0, k_heads = r.k.defined() ? r.k.size(1) : 0;
+    on.check(r.wq, "wq", any.scalar_type(), 1, true);
+    on.check(r.wk, "wk", any.scalar_type(), 1, true);
+    on.check(r.inv_freq, "inv_freq", at::kFloat, 1, true);
+    on.check(r.positions, "positions", at::kLong, 1, true);
+    if ((r.wq.defined() && r.wq.size(0) != dim) || (r.wk.defined() && r.wk.size(0) != dim)) value_error("wq and wk must be [dim]");
+    if (r.positions.defined() && r.positions.size(0) != r.tokens) value_error("positions must be [tokens]");
+    if (dim > INT32_MAX || q_heads > INT32_MAX || k_heads > INT32_MAX || r.inv_freq.size(0) > INT32_MAX / 2) value_error("q, k or inv_freq: too large");
+    r.dim = static_cast<int>(dim);
+    r.q_heads = static_cast<int>(q_heads);
+    r.k_heads = static_cast<int>(k_heads);
+    r.rot = static_cast<int>(2 * r.inv_freq.size(0));
+    return r;
+}
+const at::Tensor& first_of(PyObject* a, PyObject* b) { return a == Py_None ? tensor(b, "q or k") : tensor(a, "q"); }
+
+// 0 q, 1 k, 2 wq, 3 wk, 4 inv_freq, 5 positions, 6 style, 7 eps, 8 q_out, 9 k_out, 10 stream, 11 prepare
+PyObject* qk_fwd(PyObject* const* a) {
+    const OnDevice on(first_of(a[0], a[1]), "q");
+    const Rope r = rope_args(on, a);
+    const int style = int_of(a[6], "style");
+    const double eps = real(a[7]);
+    at::Tensor qo = optional(a[8], "q_out"), ko = optional(a[9], "k_out");
+    if (!qo.defined() && r.q.defined()) qo = empty(r.q.sizes(), r.q.scalar_type(), r.q);
+    if (!ko.defined() && r.k.defined()) ko = empty(r.k.sizes(), r.k.scalar_type(), r.k);
+    const Stream st = stream_of(a[10]);
+    auto f = [=, q = heads_of(on, r.q, "q", r.q), k = heads_of(on, r.k, "k", r.k), xq = heads_of(on, qo, "q_out", r.q), xk = heads_of(on, ko, "k_out", r.k),
+              wq = ptr(r.wq), wk = ptr(r.wk), pos = static_cast<const int64_t*>(ptr(r.positions)), fr = static_cast<const float*>(ptr(r.inv_freq)),
+              tokens = r.tokens, hq = r.q_heads, hk = r.k_heads, dim = r.dim, rot = r.rot, dt = r.dt, s = st.s] {
+        return pf_qk_norm_rope_fwd(q.p, q.ld, q.s, k.p, k.ld, k.s, wq, wk, pos, fr, xq.p, xq.ld, xq.s, xk.p, xk.ld, xk.s, tokens, hq, hk, dim, rot, style,
+                                   eps, dt, s);
+    };
+    const bool prepare = truth(a[11]);
+    std::vector<at::Tensor> keep;
+    if (prepare) keep = {r.q, r.k, r.wq, r.wk, r.inv_freq, r.positions, qo, ko};
+    return issue_on(on, prepare, f, "pf_qk_norm_rope_fwd", Workspace(), std::move(keep), tuple({qo, ko}));
+}
+
+// 0 q, 1 k, 2 wq, 3 wk, 4 inv_freq, 5 positions, 6 style, 7 eps, 8 dq_out, 9 dk_out, 10 dq, 11 dk, 12 need_dw, 13 dwq, 14 dwk, 15 accumulate,
+// 16 grads_f32, 17 workspace, 18 stream, 19 prepare
+PyObject* qk_bwd(PyObject* const* a) {
+    const OnDevice on(first_of(a[0], a[1]), "q");
+    const Rope r = rope_args(on, a);
+    const at::Tensor& any = r.q.defined() ? r.q : r.k;
+    const int style = int_of(a[6], "style");
+    const double eps = real(a[7]);
+    const at::Tensor gq = optional(a[8], "dq_out"), gk = optional(a[9], "dk_out");
+    if (gq.defined() != r.q.defined() || gk.defined() != r.k.defined()) value_error("dq_out goes with q, dk_out with k");
+    at::Tensor dq = optional(a[10], "dq"), dk = optional(a[11], "dk"), dwq = optional(a[13], "dwq"), dwk = optional(a[14], "dwk");
+    if (!dq.defined() && r.q.defined()) dq = empty(r.q.sizes(), any.scalar_type(), any);
+    if (!dk.defined() && r.k.defined()) dk = empty(r.k.sizes(), any.scalar_type(), any);
+    const unsigned flags = grad_flags(a[15], a[16]);
+    const at::ScalarType wdt = (flags & PF_GRAD_F32) ? at::kFloat : any.scalar_type();
+    if (truth(a[12])) {
+        if ((flags & PF_GRAD_ACCUMULATE) && ((r.q.defined() && r.wq.defined() && !dwq.defined()) || (r.k.defined() && r.wk.defined() && !dwk.defined())))
+            value_error("accumulate=True needs the dwq and dwk to add to");
+        if (!dwq.defined() && r.q.defined() && r.wq.defined()) dwq = empty({r.dim}, wdt, any);
+        if (!dwk.defined() && r.k.defined() && r.wk.defined()) dwk = empty({r.dim}, wdt, any);
+    }
+    on.check(dwq, "dwq", wdt, 1, true);
+    on.check(dwk, "dwk", wdt, 1, true);
+    if ((dwq.defined() && dwq.size(0) != r.dim) || (dwk.defined() && dwk.size(0) != r.dim)) value_error("dwq and dwk must be [dim]");
+    const Stream st = stream_of(a[18]);
+    Workspace ws;
+    if (a[17] != Py_None || dwq.defined() || dwk.defined())
+        ws = workspace(a[17], a[17] == Py_None ? pf_qk_norm_rope_bwd_workspace(r.tokens, r.q_heads, r.k_heads, r.dim) : 0, any, st);
+    auto f = [=, q = heads_of(on, r.q, "q", r.q), k = heads_of(on, r.k, "k", r.k), yq = heads_of(on, gq, "dq_out", r.q), yk = heads_of(on, gk, "dk_out", r.k),
+              xq = heads_of(on, dq, "dq", r.q), xk = heads_of(on, dk, "dk", r.k), wq = ptr(r.wq), wk = ptr(r.wk),
+              pos = static_cast<const int64_t*>(ptr(r.positions)), fr = static_cast<const float*>(ptr(r.inv_freq)), pwq = ptr(dwq), pwk = ptr(dwk),
+              tokens = r.tokens, hq = r.q_heads, hk = r.k_heads, dim = r.dim, rot = r.rot, dt = r.dt, wp = ws.p, wb = ws.bytes, s = st.s] {
+        return pf_qk_norm_rope_bwd(q.p, q.ld, q.s, k.p, k.ld, k.s, wq, wk, pos, fr, yq.p, yq.ld, yq.s, yk.p, yk.ld, yk.s, xq.p, xq.ld, xq.s, xk.p, xk.ld,
+                                   xk.s, pwq, pwk, tokens, hq, hk, dim, rot, style, eps, dt, flags, wp, wb, s);
+    };
+    const bool prepare = truth(a[19]);
+    std::vector<at::Tensor> keep;
+    if (prepare) keep = {r.q, r.k, r.wq, r.wk, r.inv_freq, r.positions, gq, gk, dq, dk, dwq, dwk};
+    return issue_on(on, prepare, f, "pf_qk_norm_rope_bwd", std::move(ws), std::move(keep), tuple({dq, dk, dwq, dwk}));
+}
+
+int32_t* ints(const at::Tensor& t) { return static_cast<int32_t*>(ptr(t)); }
+float* floats(const at::Tensor& t) { return static_cast<float*>(ptr(t)); }
+void expect(bool ok, const char* what) {
+    if (!ok) value_error(what);
+}
+// A matrix argument [rows, cols] (rows and cols -1: any) of the call's dtype, at any pitch.
+int64_t matrix(const OnDevice& on, const at::Tensor& t, const char* name, at::ScalarType type, int64_t rows, int64_t cols) {
+    if (!t.defined()) return 0;
+    on.check(t, name, type, 2, false);
+    if ((rows >= 0 && t.size(0) != rows) || (cols >= 0 && t.size(1) != cols)) value_error(std::string(name) + ": does not fit the other matrices");
+    return pitch(t, name);
+}
+
+// 0 ids, 1 experts, 2 capacity, 3 slots, 4 sources, 5 counts, 6 offsets, 7 stream, 8 prepare
+PyObject* expert_sort(PyObject* const* a) {
+    const at::Tensor& ids = tensor(a[0], "ids");
+    const OnDevice on(ids, "ids");
+    on.check(ids, "ids", at::kInt, 2, true);
+    const int experts = int_of(a[1], "experts");
+    const int64_t capacity = integer(a[2]), tokens = ids.size(0);
+    expect(ids.size(1) <= INT32_MAX, "ids: too large");
+    const int k = static_cast<int>(ids.size(1));
+    expect(experts >= 1 && experts < INT32_MAX && capacity >= 0 && capacity <= INT32_MAX && k >= 1,
+           "need at least one expert and one choice, and a capacity from 0 on");
+    const int64_t rows = pf_expert_rows(tokens, k, experts, capacity);
+    at::Tensor slots = optional(a[3], "slots"), sources = optional(a[4], "sources"), counts = optional(a[5], "counts"), offsets = optional(a[6], "offsets");
+    if (!slots.defined()) slots = empty({tokens, k}, at::kInt, ids);
+    if (!sources.defined()) sources = empty({rows}, at::kInt, ids);
+    if (!counts.defined()) counts = empty({experts}, at::kInt, ids);
+    if (!offsets.defined()) offsets = empty({experts + 1}, at::kInt, ids);
+    on.check(slots, "slots", at::kInt, 2, true);
+    on.check(sources, "sources", at::kInt, 1, true);
+    on.check(counts, "counts", at::kInt, 1, true);
+    on.check(offsets, "offsets", at::kInt, 1, true);
+    expect(slots.sizes() == ids.sizes() && sources.size(0) == rows && counts.size(0) == experts && offsets.size(0) == experts + 1,
+           "slots must be as ids, sources [rows], counts [experts], offsets [experts + 1]");
+    const Stream st = stream_of(a[7]);
+    auto f = [=, pi = ints(ids), ps = ints(slots), pr = ints(sources), pc = ints(counts), po = ints(offsets), s = st.s] {
+        return pf_expert_sort(pi, tokens, k, experts, capacity, ps, pr, pc, po, s);
+    };
+    const bool prepare = truth(a[8]);
+    std::vector<at::Tensor> keep;
+    if (prepare) keep = {ids, slots, sources, counts, offsets};
+    return issue_on(on, prepare, f, "pf_expert_sort", Workspace(), std::move(keep), tuple({slots, sources, counts, offsets}));
+}
+
+struct Choice {
+    int64_t tokens;
+    int k;
+};
+Choice choice(const OnDevice& on, const at::Tensor& slots, const at::Tensor& sources, int64_t rows) {
+    on.check(slots, "slots", at::kInt, 2, true);
+    on.check(sources, "sources", at::kInt, 1, true);
+    expect(slots.size(1) <= INT32_MAX, "slots: too large");
+    expect(!sources.defined() || sources.size(0) == rows, "sources: one for each row is needed");
+    return {slots.size(0), static_cast<int>(slots.size(1))};
+}
+
+// 0 x, 1 slots, 2 sources, 3 xs, 4 stream, 5 prepare
+PyObject* expert_dispatch_fwd(PyObject* const* a) {
+    const at::Tensor& x = tensor(a[0], "x");
+    const at::Tensor& slots = tensor(a[1], "slots");
+    const at::Tensor& sources = tensor(a[2], "sources");
+    const OnDevice on(x, "x");
+    const int dt = dtype_code(x);
+    expect(sources.dim() == 1, "sources: need [rows]");
+    const int64_t rows = sources.size(0);
+    const Choice c = choice(on, slots, sources, rows);
+    const int64_t ldx = matrix(on, x, "x", x.scalar_type(), c.tokens, -1), width = x.size(1);
+    at::Tensor xs = optional(a[3], "xs");
+    if (!xs.defined()) xs = empty({rows, width}, x.scalar_type(), x);
+    const int64_t ldxs = matrix(on, xs, "xs", x.scalar_type(), rows, width);
+    const Stream st = stream_of(a[4]);
+    auto f = [=, px = ptr(x), ps = ints(slots), pr = ints(sources), py = ptr(xs), s = st.s] {
+        return pf_expert_dispatch_fwd(px, ldx, ps, pr, py, ldxs, c.tokens, c.k, rows, width, dt, s);
+    };
+    const bool prepare = truth(a[5]);
+    std::vector<at::Tensor> keep;
+    if (prepare) keep = {x, slots, sources, xs};
+    return issue_on(on, prepare, f, "pf_expert_dispatch_fwd", Workspace(), std::move(keep), wrap(xs));
+}
+
+// 0 ys (dxs), 1 slots, 2 weights (None: ones), 3 y (dx), 4 stream, 5 prepare, 6 backward of dispatch
+PyObject* expert_combine_fwd(PyObject* const* a) {
+    const bool backward = truth(a[6]);
+    const at::Tensor& ys = tensor(a[0], backward ? "dxs" : "ys");
+    const at::Tensor& slots = tensor(a[1], "slots");
+    const at::Tensor weights = optional(a[2], "weights");
+    const OnDevice on(ys, backward ? "dxs" : "ys");
+    const int dt = dtype_code(ys);
+    const int64_t ldys = matrix(on, ys, backward ? "dxs" : "ys", ys.scalar_type(), -1, -1), rows = ys.size(0), width = ys.size(1);
+    const Choice c = choice(on, slots, at::Tensor(), rows);
+    on.check(weights, "weights", at::kFloat, 2, true);
+    expect(!weights.defined() || weights.sizes() == slots.sizes(), "weights must be as slots");
+    at::Tensor y = optional(a[3], backward ? "dx" : "y");
+    if (!y.defined()) y = empty({c.tokens, width}, ys.scalar_type(), ys);
+    const int64_t ldy = matrix(on, y, backward ? "dx" : "y", ys.scalar_type(), c.tokens, width);
+    const Stream st = stream_of(a[4]);
+    auto f = [=, py = ptr(ys), ps = ints(slots), pw = floats(weights), po = ptr(y), s = st.s] {
+        return backward ? pf_expert_dispatch_bwd(py, ldys, ps, po, ldy, c.tokens, c.k, rows, width, dt, s)
+                        : pf_expert_combine_fwd(py, ldys, ps, pw, po, ldy, c.tokens, c.k, rows, width, dt, s);
+    };
+    const bool prepare = truth(a[5]);
+    std::vector<at::Tensor> keep;
+    if (prepare) keep = {ys, slots, weights, y};
+    return issue_on(on, prepare, f, backward ? "pf_expert_dispatch_bwd" : "pf_expert_combine_fwd", Workspace(), std::move(keep), wrap(y));
+}
+
+// 0 ys, 1 slots, 2 sources, 3 weights, 4 dy, 5 need_dys, 6 dys, 7 need_dweights, 8 dweights, 9 stream, 10 prepare
+PyObject* expert_combine_bwd(PyObject* const* a) {
+    const at::Tensor& ys = tensor(a[0], "ys");
+    const at::Tensor& slots = tensor(a[1], "slots");
+    const at::Tensor& sources = tensor(a[2], "sources");
+    const at::Tensor& weights = tensor(a[3], "weights");
+    const at::Tensor& dy = tensor(a[4], "dy");
+    const OnDevice on(ys, "ys");
+    const int dt = dtype_code(ys);
+    const int64_t ldys = matrix(on, ys, "ys", ys.scalar_type(), -1, -1), rows = ys.size(0), width = ys.size(1);
+    const Choice c = choice(on, slots, sources, rows);
+    on.check(weights, "weights", at::kFloat, 2, true);
+    expect(weights.sizes() == slots.sizes(), "weights must be as slots");
+    const int64_t lddy = matrix(on, dy, "dy", ys.scalar_type(), c.tokens, width);
+    at::Tensor dys = optional(a[6], "dys"), dw = optional(a[8], "dweights");
+    if (!dys.defined() && truth(a[5])) dys = empty({rows, width}, ys.scalar_type(), ys);
+    if (!dw.defined() && truth(a[7])) dw = empty(slots.sizes(), at::kFloat, ys);
+    const int64_t lddys = matrix(on, dys, "dys", ys.scalar_type(), rows, width);
+    on.check(dw, "dweights", at::kFloat, 2, true);
+    expect(!dw.defined() || dw.sizes() == slots.sizes(), "dweights must be as slots");
+    const Stream st = stream_of(a[9]);
+    auto f = [=, py = ptr(ys), ps = ints(slots), pr = ints(sources), pw = floats(weights), pg = ptr(dy), pd = ptr(dys), pdw = floats(dw), s = st.s] {
+        return pf_expert_combine_bwd(py, ldys, ps, pr, pw, pg, lddy, pd, lddys, pdw, c.tokens, c.k, rows, width, dt, s);
+    };
+    const bool prepare = truth(a[10]);
+    std::vector<at::Tensor> keep;
+    if (prepare) keep = {ys, slots, sources, weights, dy, dys, dw};
+    return issue_on(on, prepare, f, "pf_expert_combine_bwd", Workspace(), std::move(keep), tuple({dys, dw}));
+}
+
+// The contiguous tensors of a list that goes with the parameters: numels[i] elements each, or one for each 256 of them.
+template <typename P>
+std::vector<P> array_list(PyObject* seq, const char* name, const OnDevice& on, at::ScalarType type, const std::vector<int64_t>& numels, bool scales,
+                          std::vector<at::Tensor>* keep) {
+    std::vector<P> out;
+    if (seq == Py_None) return out;
+    PyObject* fast = PySequence_Fast(seq, "need sequences of tensors");
+    if (!fast) throw python_error();
+    struct Drop { PyObject* o; ~Drop() { Py_DECREF(o); } } drop{fast};
+    const size_t n = static_cast<size_t>(PySequence_Fast_GET_SIZE(fast));
+    if (n != numels.size()) value_error(std::string(name) + ": need one tensor for each parameter");
+    out.resize(n);
+    for (size_t i = 0; i < n; ++i) {
+        const at::Tensor& t = tensor(PySequence_Fast_GET_ITEM(fast, static_cast<Py_ssize_t>(i)), name);
+        if (t.device() != on.device || t.scalar_type() != type || !t.is_contiguous() || t.numel() != (scales ? (numels[i] + 255) / 256 : numels[i]))
+            value_error(std::string(name) + ": need contiguous " + c10::toString(type) + " tensors on " + on.device.str() +
+                        (scales ? " of one element for each 256 of the parameter" : " of as many elements as the parameter"));
+        out[i] = static_cast<P>(t.data_ptr());
+        if (keep) keep->push_back(t);
+    }
+    return out;
+}
+
+// 0 params (not empty), 1 grads, 2 m, 3 v, 4 masters, 5 m_scales, 6 v_scales, 7 lr, 8 beta1, 9 beta2, 10 eps, 11 weight_decay, 12 step, 13 grad_scale,
+// 14 seed, 15 scalars, 16 stream, 17 prepare
+PyObject* adamw_step(PyObject* const* a) {
+    PyObject* fast = PySequence_Fast(a[0], "params: need a sequence of tensors");
+    if (!fast) throw python_error();
+    struct Drop { PyObject* o; ~Drop() { Py_DECREF(o); } } drop{fast};
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(fast);
+    const at::Tensor& first = tensor(PySequence_Fast_GET_ITEM(fast, 0), "params");
+    const OnDevice on(first, "params");
+    const int pdt = dtype_code(first);
+    std::vector<int64_t> n(static_cast<size_t>(count));
+    for (Py_ssize_t i = 0; i < count; ++i) n[i] = tensor(PySequence_Fast_GET_ITEM(fast, i), "params").numel();
+    auto first_type = [&](PyObject* seq, const char* name) {
+        PyObject* o = PySequence_GetItem(seq, 0);
+        if (!o) throw python_error();
+        struct Hold { PyObject* o; ~Hold() { Py_DECREF(o); } } hold{o};
+        return tensor(o, name).scalar_type();
+    };
+    const at::ScalarType gt = first_type(a[1], "grads"), mt = first_type(a[2], "m");
+    if (gt != at::kFloat && gt != at::kBFloat16) throw PyError{PyExc_TypeError, std::string("grads: unsupported dtype ") + c10::toString(gt)};
+    const bool state8 = mt == at::kFloat8_e4m3fn;
+    if (!state8 && mt != at::kFloat) throw PyError{PyExc_TypeError, std::string("m: unsupported dtype ") + c10::toString(mt)};
+    if (state8 != (a[5] != Py_None) || state8 != (a[6] != Py_None)) value_error("m_scales and v_scales go with states in 8 bits (m float8_e4m3fn, v float8_e5m2)");
+    if (a[4] != Py_None && pdt != PF_BF16) value_error("masters go with bfloat16 parameters");
+    const bool prepare = truth(a[17]);
+    std::vector<at::Tensor> keep;
+    std::vector<at::Tensor>* const k = prepare ? &keep : nullptr;
+    auto params = array_list<void*>(fast, "params", on, first.scalar_type(), n, false, k);
+    auto grads = array_list<const void*>(a[1], "grads", on, gt, n, false, k);
+    auto m = array_list<void*>(a[2], "m", on, mt, n, false, k);
+    auto v = array_list<void*>(a[3], "v", on, state8 ? at::kFloat8_e5m2 : at::kFloat, n, false, k);
+    auto masters = array_list<float*>(a[4], "masters", on, at::kFloat, n, false, k);
+    auto ms = array_list<float*>(a[5], "m_scales", on, at::kFloat, n, true, k);
+    auto vs = array_list<float*>(a[6], "v_scales", on, at::kFloat, n, true, k);
+    if (v.empty()) value_error("v: need one tensor for each parameter");
+    pf_adamw h;
+    h.lr = real(a[7]); h.beta1 = real(a[8]); h.beta2 = real(a[9]); h.eps = real(a[10]); h.weight_decay = real(a[11]);
+    h.step = integer(a[12]);
+    h.grad_scale = static_cast<float>(real(a[13]));
+    const int64_t seed = integer(a[14]);
+    if (seed < 0 || seed > 0xffffffffLL) value_error("seed: need 0 .. 2^32 - 1");
+    h.seed = static_cast<uint32_t>(seed);
+    const at::Tensor scalars = optional(a[15], "scalars");
+    on.check(scalars, "scalars", at::kFloat, 1, true);
+    if (scalars.defined() && scalars.size(0) != 5) value_error("scalars: need the five of pf_adamw_scalars");
+    if (prepare && scalars.defined()) keep.push_back(scalars);
+    const Stream st = stream_of(a[16]);
+    const int gdt = gt == at::kBFloat16 ? PF_BF16 : PF_F32, state = state8 ? PF_STATE_8BIT : PF_STATE_F32, c = static_cast<int>(count);
+    auto f = [=, params = std::move(params), grads = std::move(grads), m = std::move(m), v = std::move(v), masters = std::move(masters), ms = std::move(ms),
+              vs = std::move(vs), n = std::move(n), sc = static_cast<const pf_adamw_scalars*>(ptr(scalars)), s = st.s] {
+        return pf_adamw_step(params.data(), masters.empty() ? nullptr : masters.data(), grads.data(), m.data(), v.data(), ms.empty() ? nullptr : ms.data(),
+                             vs.empty() ? nullptr : vs.data(), n.data(), c, pdt, gdt, state, &h, sc, s);
+    };
+    Py_INCREF(Py_None);
+    return issue_on(on, prepare, std::move(f), "pf_adamw_step", Workspace(), std::move(keep), Py_None);
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
     Py_INCREF(cls);
     Py_XSETREF(g_pf_error, cls);
@@ -575,7 +939,9 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 #define PF_ENTRY(name, args) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<name, args>)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {PF_ENTRY(linear_fwd, 12), PF_ENTRY(linear_fwd_static, 6), PF_ENTRY(linear_bwd, 14), PF_ENTRY(bias_act_bwd, 7),
                            PF_ENTRY(grouped_fwd, 9), PF_ENTRY(grouped_bwd, 12), PF_ENTRY(conv_fwd, 11), PF_ENTRY(conv_bwd, 16),
-                           PF_ENTRY(pack, 4), PF_ENTRY(unpack, 3), {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                           PF_ENTRY(pack, 4), PF_ENTRY(unpack, 3), PF_ENTRY(qk_fwd, 12), PF_ENTRY(qk_bwd, 20),
+                           PF_ENTRY(expert_sort, 9), PF_ENTRY(expert_dispatch_fwd, 6), PF_ENTRY(expert_combine_fwd, 7), PF_ENTRY(expert_combine_bwd, 11),
+                           PF_ENTRY(adamw_step, 18), {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_pf_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
