@@ -464,8 +464,9 @@ int pf_expert_sort(const int32_t* ids, int64_t tokens, int k, int experts, int64
         return PF_ERR_INVALID_ARG;
     const SortParams p{ids, slots, sources, counts, offsets, static_cast<int>(a), experts, static_cast<int>(capacity), static_cast<int>(rows)};
     const size_t smem = sizeof(int) * static_cast<size_t>(experts) * (kSortWarps + 3);      // 152 KB for the most experts
+    static std::atomic<uint64_t> allowed{0};
     if (smem > 48 * 1024)
-        PF_CUDA(cudaFuncSetAttribute(reinterpret_cast<const void*>(&sort_kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+        PF_CUDA(allow_dynamic_smem(reinterpret_cast<const void*>(&sort_kernel), sizeof(int) * kMostExperts * (kSortWarps + 3), allowed));
     int blocks = 1;
     while (blocks < kSortBlocks && static_cast<int64_t>(blocks) * kSortThreads < a) blocks *= 2;
     PF_CUDA(launch_beside(sort_kernel, dim3(static_cast<unsigned>(blocks)), kSortThreads, smem, blocks, static_cast<cudaStream_t>(cuda_stream), p));

@@ -7,6 +7,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "pf.h"
 
 namespace pf {
@@ -167,6 +169,18 @@ int linear_fwd_impl(const void* x, int64_t ldx, const void* U, int64_t ldu, cons
 
 // host-side count of kernels launched by this library
 void count_launch(int n = 1);
+
+// Raises a kernel's limit of dynamic shared memory; `done` remembers the devices on which that has been done.
+inline cudaError_t allow_dynamic_smem(const void* kernel, size_t bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    const cudaError_t g = cudaGetDevice(&dev);
+    if (g != cudaSuccess) return g;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
+}
 
 // A launch that may start beside the tail of the one before in its stream: its kernel executes griddepcontrol.wait before it touches
 // global memory.  cluster > 1: blocks of a cluster, along x.

@@ -114,12 +114,44 @@ __device__ __forceinline__ float sum_lanes(float x) {
     return x;
 }
 
-// kLanes lanes to a row (the power of two from the row's pieces / 2 on), 32 / kLanes rows of a warp at a time.
+// The rows that a warp takes one after the other: kRows heads at a time of the units of (token, some of its heads) that are its share.
+struct RopeWalk {
+    int64_t token;
+    int part, h, end;      // the unit's place among its token's, the next head, the first behind the unit
+    __device__ __forceinline__ bool valid(const RopeParams& p) const { return token < p.tokens; }
+    __device__ __forceinline__ void enter(const RopeSide& s) {
+        h = part * s.heads_per_unit;
+        end = min(h + s.heads_per_unit, s.heads);
+    }
+    __device__ __forceinline__ void start(const RopeSide& s, int64_t unit) {
+        token = unit / s.units_per_token;
+        part = static_cast<int>(unit - token * s.units_per_token);
+        enter(s);
+    }
+    // The next unit is step_tokens tokens and step_parts parts on.
+    __device__ __forceinline__ void next_unit(const RopeSide& s, int64_t step_tokens, int step_parts) {
+        token += step_tokens;
+        part += step_parts;
+        if (part >= s.units_per_token) { part -= s.units_per_token; ++token; }
+        enter(s);
+    }
+};
+
+__device__ __forceinline__ void fetch16(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+
+// kLanes lanes to a row (the power of two from the row's pieces / 2 on), 32 / kLanes rows of a warp at a time.  Each lane keeps the
+// pieces of its next kStages - 1 rows on the way into its own places of shared memory, across units: what a warp waits for was asked for rows
+// ago, and nothing is exchanged between lanes but the sums.
+template <bool kBwd> constexpr int kRopeStages = kBwd ? 4 : 6;
+template <bool kBwd> constexpr int kRopePieces = kBwd ? 4 : 2;      // 16-byte pieces of a lane for a row: two of x, two of the gradient
+template <bool kBwd> constexpr int kRopeRing = kRopeWarps * kRopeStages<kBwd> * kRopePieces<kBwd> * 32 * 16;
+
 template <typename T, int kLanes, bool kPairs, bool kBwd>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) {
-    constexpr int kN = Piece<T>::kN, kRows = 32 / kLanes, kDeep = kBwd ? 1 : 2;
-    __shared__ float2 cs_smem[kRopeWarps][kMaxPairs];
-    __shared__ float red[kBwd ? kRopeWarps * 2 * kN * kLanes : 1];
+__global__ void __launch_bounds__(kRopeThreads, kBwd ? 2 : 3) rope_kernel(const RopeParams p) {
+    constexpr int kN = Piece<T>::kN, kRows = 32 / kLanes, kStages = kRopeStages<kBwd>, kPieces = kRopePieces<kBwd>;
+    extern __shared__ __align__(16) unsigned char rope_smem[];      // the lanes' pieces, then each warp's angles
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bool key = static_cast<int>(blockIdx.x) >= p.side[0].blocks;
     const RopeSide& s = p.side[key ? 1 : 0];
@@ -128,8 +160,41 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) 
     const int l = lane % kLanes, row = lane / kLanes, half = p.rot / 2;
     const bool there = 2 * kN * l < p.dim, turned = kN * l < half;
     const int ia = turned ? kN * l : p.rot + kN * l - half, ib = ia + (turned ? half : (p.dim - p.rot) / 2);
+    unsigned char* const ring = rope_smem + (warp * kStages * kPieces * 32 + lane) * 16;
+    const uint32_t ring_at = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
+    float2* const angles = reinterpret_cast<float2*>(rope_smem + kRopeRing<kBwd>) + warp * half;
+    const int64_t step = static_cast<int64_t>(s.blocks) * kRopeWarps, step_tokens = step / s.units_per_token;
+    const int step_parts = static_cast<int>(step - step_tokens * s.units_per_token);
+    RopeWalk ahead, at;      // rows to ask for, rows to compute
+    ahead.start(s, static_cast<int64_t>(block) * kRopeWarps + warp);
+    at = ahead;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const T* const xs = static_cast<const T*>(s.x);
+    const T* const gs = static_cast<const T*>(s.g);
+    auto ask = [&](int stage) {
+        if (ahead.valid(p)) {
+            const int64_t head = ahead.h + row;
+            if (there && head < ahead.end) {
+                const uint32_t to = ring_at + stage * (kPieces * 32 * 16);
+                const T* const x = xs + ahead.token * s.ldx + head * s.sx;
+                fetch16(to, x + ia);
+                fetch16(to + 512, x + ib);
+                if constexpr (kBwd) {
+                    const T* const g = gs + ahead.token * s.ldg + head * s.sg;
+                    fetch16(to + 1024, g + ia);
+                    fetch16(to + 1536, g + ib);
+                }
+            }
+            ahead.h += kRows;
+            if (ahead.h >= ahead.end) ahead.next_unit(s, step_tokens, step_parts);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) ask(i);
+    auto position_of = [&](const RopeWalk& w) { return !w.valid(p) ? 0 : p.positions ? p.positions[w.token] : w.token; };
+    int64_t position = position_of(at);
     float wa[kN], wb[kN];
 #pragma unroll
     for (int i = 0; i < kN; ++i) wa[i] = wb[i] = 1.f;
@@ -144,91 +209,90 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) 
 #pragma unroll
     for (int i = 0; i < kN; ++i) dwa[i] = dwb[i] = 0.f;
     const float inv_dim = 1.f / static_cast<float>(p.dim);
-    const int64_t units = p.tokens * s.units_per_token;
-    for (int64_t unit = static_cast<int64_t>(block) * kRopeWarps + warp; unit < units; unit += static_cast<int64_t>(s.blocks) * kRopeWarps) {
-        const int64_t token = unit / s.units_per_token;
-        const int head0 = static_cast<int>(unit % s.units_per_token) * s.heads_per_unit;
-        const int head1 = min(head0 + s.heads_per_unit, s.heads);
-        const int64_t position = p.positions ? p.positions[token] : token;
+    int stage = 0;
+    while (at.valid(p)) {
         __syncwarp();
-        for (int i = lane; i < half; i += 32) cs_smem[warp][i] = turn_of(position, p.inv_freq[i]);
+        for (int i = lane; i < half; i += 32) angles[i] = turn_of(position, p.inv_freq[i]);
         __syncwarp();
         float2 cs[kN];
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
             const int pair = kPairs ? (i < kN / 2 ? ia / 2 + i : ib / 2 + i - kN / 2) : ia + i;
-            cs[i] = turned ? cs_smem[warp][pair] : make_float2(1.f, 0.f);
+            cs[i] = turned ? angles[pair] : make_float2(1.f, 0.f);
         }
-        const T* const x = static_cast<const T*>(s.x) + token * s.ldx;
-        T* const out = static_cast<T*>(s.out) + token * s.ldo;
-        for (int h = head0; h < head1; h += kRows * kDeep) {
-            Piece<T> xa[kDeep], xb[kDeep], ga, gb;
-            bool on[kDeep];
-#pragma unroll
-            for (int u = 0; u < kDeep; ++u) {
-                const int64_t head = h + u * kRows + row;
-                on[u] = there && head < head1;
-                xa[u].raw = {};
-                xb[u].raw = {};
-                if (on[u]) {
-                    xa[u].load(x + head * s.sx + ia);
-                    xb[u].load(x + head * s.sx + ib);
-                }
+        RopeWalk next = at;
+        next.next_unit(s, step_tokens, step_parts);
+        position = position_of(next);
+        T* const out = static_cast<T*>(s.out) + at.token * s.ldo;
+        for (; at.h < at.end; at.h += kRows) {
+            __syncwarp();
+            ask(stage == 0 ? kStages - 1 : stage - 1);      // the place that the row before has left
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+            const unsigned char* const in = ring + stage * (kPieces * 32 * 16);
+            stage = stage == kStages - 1 ? 0 : stage + 1;
+            const int64_t head = at.h + row;
+            const bool live = head < at.end, on = there && live;
+            float a[kN], b[kN];
+            Piece<T> xa, xb;
+            xa.raw = {};
+            xb.raw = {};
+            if (on) {
+                xa.load(reinterpret_cast<const T*>(in));
+                xb.load(reinterpret_cast<const T*>(in + 512));
             }
-            if constexpr (kBwd) {
+            xa.get(a);
+            xb.get(b);
+            float sq = 0.f;
+#pragma unroll
+            for (int i = 0; i < kN; ++i) sq = fmaf(a[i], a[i], fmaf(b[i], b[i], sq));
+            sq = sum_lanes<kLanes>(sq);
+            // (a row behind the last head adds nothing to dw, whatever eps is)
+            const float r = live ? rsqrtf(fmaf(sq, inv_dim, p.eps)) : 0.f;
+            if constexpr (!kBwd) {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) { a[i] *= r * wa[i]; b[i] *= r * wb[i]; }
+                turn<kN, kPairs>(a, b, cs, 1.f);
+            } else {
+                Piece<T> ga, gb;
                 ga.raw = {};
                 gb.raw = {};
-                if (on[0]) {
-                    const T* const g = static_cast<const T*>(s.g) + token * s.ldg + (h + row) * s.sg;
-                    ga.load(g + ia);
-                    gb.load(g + ib);
+                if (on) {
+                    ga.load(reinterpret_cast<const T*>(in + 1024));
+                    gb.load(reinterpret_cast<const T*>(in + 1536));
                 }
+                float ea[kN], eb[kN], dot = 0.f;
+                ga.get(ea);
+                gb.get(eb);
+                turn<kN, kPairs>(ea, eb, cs, -1.f);
+#pragma unroll
+                for (int i = 0; i < kN; ++i) {
+                    a[i] *= r;
+                    b[i] *= r;
+                    dwa[i] = fmaf(ea[i], a[i], dwa[i]);
+                    dwb[i] = fmaf(eb[i], b[i], dwb[i]);
+                    ea[i] *= wa[i];
+                    eb[i] *= wb[i];
+                    dot = fmaf(ea[i], a[i], fmaf(eb[i], b[i], dot));
+                }
+                dot = sum_lanes<kLanes>(dot) * inv_dim;
+#pragma unroll
+                for (int i = 0; i < kN; ++i) { a[i] = r * (ea[i] - a[i] * dot); b[i] = r * (eb[i] - b[i] * dot); }
             }
-#pragma unroll
-            for (int u = 0; u < kDeep; ++u) {
-                float a[kN], b[kN];
-                xa[u].get(a);
-                xb[u].get(b);
-                float sq = 0.f;
-#pragma unroll
-                for (int i = 0; i < kN; ++i) sq = fmaf(a[i], a[i], fmaf(b[i], b[i], sq));
-                sq = sum_lanes<kLanes>(sq);
-                // (a row behind the last head adds nothing to dw, whatever eps is)
-                const float r = h + u * kRows + row < head1 ? rsqrtf(fmaf(sq, inv_dim, p.eps)) : 0.f;
-                if constexpr (!kBwd) {
-#pragma unroll
-                    for (int i = 0; i < kN; ++i) { a[i] *= r * wa[i]; b[i] *= r * wb[i]; }
-                    turn<kN, kPairs>(a, b, cs, 1.f);
-                } else {
-                    float ea[kN], eb[kN], dot = 0.f;
-                    ga.get(ea);
-                    gb.get(eb);
-                    turn<kN, kPairs>(ea, eb, cs, -1.f);
-#pragma unroll
-                    for (int i = 0; i < kN; ++i) {
-                        a[i] *= r;
-                        b[i] *= r;
-                        dwa[i] = fmaf(ea[i], a[i], dwa[i]);
-                        dwb[i] = fmaf(eb[i], b[i], dwb[i]);
-                        ea[i] *= wa[i];
-                        eb[i] *= wb[i];
-                        dot = fmaf(ea[i], a[i], fmaf(eb[i], b[i], dot));
-                    }
-                    dot = sum_lanes<kLanes>(dot) * inv_dim;
-#pragma unroll
-                    for (int i = 0; i < kN; ++i) { a[i] = r * (ea[i] - a[i] * dot); b[i] = r * (eb[i] - b[i] * dot); }
-                }
-                if (on[u]) {
-                    const int64_t head = h + u * kRows + row;
-                    Piece<T>::store(out + head * s.so + ia, a);
-                    Piece<T>::store(out + head * s.so + ib, b);
-                }
+            if (on) {
+                T* const o = out + head * s.so;
+                Piece<T>::store(o + ia, a);
+                Piece<T>::store(o + ib, b);
             }
         }
+        at = next;
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     if constexpr (kBwd) {
         if (!s.partial) return;
         // rows of a warp, then warps in order
+        float* const red = reinterpret_cast<float*>(rope_smem);      // (16 KB of the pieces' places at most)
+        static_assert(kRopeWarps * 2 * kN * kLanes * 4 <= kRopeRing<kBwd>, "");
+        __syncthreads();
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
 #pragma unroll
@@ -378,8 +442,9 @@ struct RopePlan {
     int lanes, warps;            // lanes of a row, warps of a block
     int blocks[2], heads_per_unit[2], units_per_token[2];
 };
-constexpr int kRopeBlocksPerSm = 4;
-RopePlan rope_plan(int64_t tokens, const int (&heads)[2], int dim, int rot, int dtype, bool pieces) {
+// Blocks of an SM: what its shared memory holds of the vector kernels (64 and 80 KB each with the most angles), and as many of the others.
+constexpr int rope_blocks_per_sm(bool bwd) { return bwd ? 2 : 3; }
+RopePlan rope_plan(int64_t tokens, const int (&heads)[2], int dim, int rot, int dtype, bool pieces, bool bwd) {
     RopePlan pl = {};
     const int n = 16 / static_cast<int>(dtype_size(dtype));
     pl.pieces = pieces && dim % (2 * n) == 0 && rot % (2 * n) == 0 && dim / (2 * n) <= 32 && rot / 2 <= kMaxPairs;
@@ -388,7 +453,7 @@ RopePlan rope_plan(int64_t tokens, const int (&heads)[2], int dim, int rot, int 
         for (pl.lanes = 2; pl.lanes < dim / (2 * n);) pl.lanes *= 2;
     pl.warps = pl.pieces ? kRopeWarps : kAnyWarps;
     const int rows = pl.pieces ? 32 / pl.lanes : 1, all = heads[0] + heads[1];
-    const int64_t most = static_cast<int64_t>(num_sms()) * kRopeBlocksPerSm;
+    const int64_t most = static_cast<int64_t>(num_sms()) * rope_blocks_per_sm(bwd) * (pl.pieces ? 1 : 2);
     for (int i = 0; i < 2; ++i) {
         if (heads[i] == 0) continue;
         // all heads of a token in one unit, unless that leaves warps without any
@@ -403,10 +468,17 @@ RopePlan rope_plan(int64_t tokens, const int (&heads)[2], int dim, int rot, int 
     return pl;
 }
 
+template <typename T, int kLanes, bool kPairs, bool kBwd>
+cudaError_t rope_styled(const RopeParams& p, int blocks, cudaStream_t stream) {
+    static std::atomic<uint64_t> allowed{0};
+    const auto kernel = rope_kernel<T, kLanes, kPairs, kBwd>;
+    const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), kRopeRing<kBwd> + kRopeWarps * kMaxPairs * sizeof(float2), allowed);
+    if (e != cudaSuccess) return e;
+    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kRopeThreads, kRopeRing<kBwd> + kRopeWarps * (p.rot / 2) * sizeof(float2), 1, stream, p);
+}
 template <typename T, int kLanes, bool kBwd>
 cudaError_t rope_pieces(const RopeParams& p, bool pairs, int blocks, cudaStream_t stream) {
-    const auto kernel = pairs ? rope_kernel<T, kLanes, true, kBwd> : rope_kernel<T, kLanes, false, kBwd>;
-    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kRopeThreads, 0, 1, stream, p);
+    return pairs ? rope_styled<T, kLanes, true, kBwd>(p, blocks, stream) : rope_styled<T, kLanes, false, kBwd>(p, blocks, stream);
 }
 template <typename T, bool kBwd>
 cudaError_t rope_launch(const RopeParams& p, const RopePlan& pl, bool pairs, cudaStream_t stream) {
@@ -460,7 +532,7 @@ int pf_qk_norm_rope_fwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
     for (int i = 0; i < 2; ++i)
         if (heads[i] > 0)
             pieces = pieces && rows_in_pieces(x[i], dtype) && rows_in_pieces(out[i], dtype) && reinterpret_cast<uintptr_t>(w[i]) % 16 == 0;
-    const RopePlan pl = rope_plan(tokens, heads, dim, rot_dim, dtype, pieces);
+    const RopePlan pl = rope_plan(tokens, heads, dim, rot_dim, dtype, pieces, false);
     RopeParams p = {};
     p.positions = positions;
     p.inv_freq = inv_freq;
@@ -480,7 +552,7 @@ int pf_qk_norm_rope_fwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
 size_t pf_qk_norm_rope_bwd_workspace(int64_t tokens, int q_heads, int k_heads, int dim) {
     if (tokens <= 0 || q_heads < 0 || k_heads < 0 || dim < 1) return 0;
     // a row of sums for each block, of which there are at most so many on either side
-    return align_up(sizeof(float) * dim * (static_cast<size_t>(num_sms()) * kRopeBlocksPerSm + 2), 256);
+    return align_up(sizeof(float) * dim * (static_cast<size_t>(num_sms()) * 2 * rope_blocks_per_sm(true) + 2), 256);
 }
 
 int pf_qk_norm_rope_bwd(const void* q, int64_t ldq, int64_t sq, const void* k, int64_t ldk, int64_t sk, const void* wq, const void* wk,
@@ -513,7 +585,7 @@ int pf_qk_norm_rope_bwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
             if (dw[i] && !(flags & PF_GRAD_ACCUMULATE)) PF_CUDA(cudaMemsetAsync(dw[i], 0, dim * dtype_size(wtype), stream));
         return PF_OK;
     }
-    const RopePlan pl = rope_plan(tokens, heads, dim, rot_dim, dtype, pieces);
+    const RopePlan pl = rope_plan(tokens, heads, dim, rot_dim, dtype, pieces, true);
     RopeParams p = {};
     p.positions = positions;
     p.inv_freq = inv_freq;
