@@ -7,8 +7,8 @@
 //
 // Bound by memory: a row is read and written once (backward: two read, one written).  A row's pair elements lie rot / 2 apart
 // (PF_ROPE_HALVES) or side by side (PF_ROPE_PAIRS); a lane takes one 16-byte piece of each half, so that both elements of a pair are
-// in one lane under either style, and a row is 2 to 32 lanes.  A warp takes several heads of a token, so that the angles (product
-// and reduction to a turn in pairs of fp64, sine and cosine in fp32) are computed once for all of them and stay in registers.
+// in one lane under either style, and a row is 2 to 32 lanes.  A warp takes several heads of a token, so that the angles (an
+// integer product in parts of a turn, sine and cosine in fp32) are computed once for all of them and stay in registers.
 #include <algorithm>
 #include <cmath>
 
@@ -31,6 +31,7 @@ struct RopeSide {
     float* partial;         // backward: one row of sums for dw per block, or null
     int64_t ldx, sx, ldg, sg, ldo, so;
     int heads, heads_per_unit, units_per_token, blocks;
+    int step_tokens, step_parts;      // from a warp's unit to its next
 };
 struct RopeParams {
     RopeSide side[2];
@@ -41,68 +42,128 @@ struct RopeParams {
     float eps;
 };
 
-// Cosine and sine of the angle position * f, position up to 2^53.  Product and turns are pairs of fp64 numbers (the second what rounding the first
-// left out), so that what remains of them after the whole turns is good to fp32 at any position; it is rounded only then.
-__device__ __forceinline__ float2 turn_of(int64_t position, float f) {
-    constexpr double kTurn = 0.15915494309189535, kTurnRest = -9.839338337591243e-18;      // 1 / (2 pi)
-    const double t = static_cast<double>(position), a = t * static_cast<double>(f), a_rest = fma(t, static_cast<double>(f), -a);
-    const double turns = a * kTurn, rest = fma(a, kTurn, -turns) + fma(a, kTurnRest, a_rest * kTurn);
+// Angles are counted in 2^-64 of a turn, modulo a turn: a position times the turn that one position takes is then an integer product, off by at most
+// 2^-64 of a turn for each position (2^-24 at position 2^40), and its upper half is the angle to 2^-32.
+//
+// The turn of one position, f / (2 pi): f's 24 bits times 1 / (2 pi) in 2^-96, moved by f's exponent (f up to 2^31; the whole turns fall off the top).
+__device__ __forceinline__ uint64_t turn_per_position(float f) {
+    constexpr uint32_t k0 = 0x28be60dbu, k1 = 0x9391054au, k2 = 0x7f09d5f4u;      // 2^96 / (2 pi)
+    const uint32_t bits = __float_as_uint(f), exponent = (bits >> 23) & 0xffu;
+    const uint32_t digits = exponent ? (bits & 0x7fffffu) | 0x800000u : 0u;
+    // digits * k: 120 bits, low (32), then high (88)
+    const uint64_t p2 = static_cast<uint64_t>(digits) * k2, p1 = static_cast<uint64_t>(digits) * k1 + (p2 >> 32);
+    const uint64_t p0 = static_cast<uint64_t>(digits) * k0 + (p1 >> 32);
+    const uint64_t low = (p1 << 32) | (p2 & 0xffffffffu);
+    // f = digits 2^(exponent - 150), so that the product is in 2^(exponent - 246) of a turn
+    const int down = 182 - static_cast<int>(exponent);
+    uint64_t turn = 0;
+    if (down >= 64) turn = down < 128 ? p0 >> (down - 64) : 0;
+    else if (down > 0) turn = (p0 << (64 - down)) | (low >> down);
+    return bits >> 31 ? 0 - turn : turn;
+}
+// Cosine and sine.  kExact: to fp32; else the hardware's approximations within half a turn, off by 2^-20.5: 2^-12 of half a step of a bf16 result
+// as large as its pair (with angles in fp64 and sincospif instead
+// the forward of 16384 x 40 heads of 128 took 70 us where it took 66 with these).
+template <bool kExact>
+__device__ __forceinline__ float2 turn_of(int64_t position, uint64_t each) {
+    const float half_turns = static_cast<float>(static_cast<int>((static_cast<uint64_t>(position) * each) >> 32)) * 0x1p-31f;
     float s, c;
-    sincospif(2.f * static_cast<float>((turns - rint(turns)) + rest), &s, &c);
+    if constexpr (kExact) {
+        sincospif(half_turns, &s, &c);
+    } else {
+        const float x = half_turns * 3.14159265f;
+        s = __sinf(x);
+        c = __cosf(x);
+    }
     return make_float2(c, s);
 }
 
-template <typename T> struct Piece;      // 16 bytes
-template <> struct Piece<float> {
-    static constexpr int kN = 4;
-    float4 raw;
-    __device__ __forceinline__ void load(const float* p) { raw = *reinterpret_cast<const float4*>(p); }
-    __device__ __forceinline__ void get(float* x) const { x[0] = raw.x; x[1] = raw.y; x[2] = raw.z; x[3] = raw.w; }
-    static __device__ __forceinline__ void store(float* p, const float* x) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
-};
-template <> struct Piece<__nv_bfloat16> {
-    static constexpr int kN = 8;
-    uint4 raw;
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) { raw = *reinterpret_cast<const uint4*>(p); }
-    __device__ __forceinline__ void get(float* x) const {
-        const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-    }
-    static __device__ __forceinline__ void store(__nv_bfloat16* p, const float* x) {
-        unsigned w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            w[i] = *reinterpret_cast<const unsigned*>(&t);
-        }
-        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-};
 __device__ __forceinline__ float get1(const float* p) { return *p; }
 __device__ __forceinline__ float get1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 __device__ __forceinline__ void put1(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put1(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
-// Turns a lane's pairs in place: a[] and b[] are its two pieces, cs its pairs in order (sine negated: turns back).
-template <int kN, bool kPairs>
-__device__ __forceinline__ void turn(float (&a)[kN], float (&b)[kN], const float2 (&cs)[kN], float sign) {
-    if constexpr (kPairs) {
+// Two fp32 numbers that one instruction works on.
+struct F2 {
+    uint64_t v;
+};
+__device__ __forceinline__ F2 f2(float x, float y) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 split(F2 a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ F2 mul(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ F2 negated(F2 a) { return F2{a.v ^ 0x8000000080000000ull}; }
+
+template <typename T> struct Piece;      // 16 bytes: kN elements, kN / 2 pairs of neighbours
+template <> struct Piece<float> {
+    static constexpr int kN = 4;
+    float4 raw;
+    __device__ __forceinline__ void load(const void* p) { raw = *static_cast<const float4*>(p); }
+    __device__ __forceinline__ void get(F2* x) const { x[0] = f2(raw.x, raw.y); x[1] = f2(raw.z, raw.w); }
+    static __device__ __forceinline__ void store(void* p, const F2* x) {
+        const float2 a = split(x[0]), b = split(x[1]);
+        *static_cast<float4*>(p) = make_float4(a.x, a.y, b.x, b.y);
+    }
+};
+template <> struct Piece<__nv_bfloat16> {
+    static constexpr int kN = 8;
+    uint4 raw;
+    __device__ __forceinline__ void load(const void* p) { raw = *static_cast<const uint4*>(p); }
+    __device__ __forceinline__ void get(F2* x) const {
+        const unsigned w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-        for (int i = 0; i < kN / 2; ++i) {
-            const float c0 = cs[i].x, s0 = sign * cs[i].y, c1 = cs[kN / 2 + i].x, s1 = sign * cs[kN / 2 + i].y;
-            const float a0 = a[2 * i], a1 = a[2 * i + 1], b0 = b[2 * i], b1 = b[2 * i + 1];
-            a[2 * i] = a0 * c0 - a1 * s0;
-            a[2 * i + 1] = a1 * c0 + a0 * s0;
-            b[2 * i] = b0 * c1 - b1 * s1;
-            b[2 * i + 1] = b1 * c1 + b0 * s1;
+        for (int i = 0; i < 4; ++i) x[i] = f2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    }
+    static __device__ __forceinline__ void store(void* p, const F2* x) {
+        unsigned w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = split(x[i]);
+            const __nv_bfloat162 t = __floats2bfloat162_rn(f.x, f.y);
+            w[i] = *reinterpret_cast<const unsigned*>(&t);
+        }
+        *static_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+
+// A lane's pairs turned in place by the angles of c and s (kBack: back).  kPairs: a pair is two neighbours, those of a[] come first in c and s; else
+// a pair is an element of a[] and one of b[].
+template <int kN, bool kPairs, bool kBack>
+__device__ __forceinline__ void turn(F2 (&a)[kN / 2], F2 (&b)[kN / 2], const F2 (&c)[kN / 2], const F2 (&s)[kN / 2]) {
+    if constexpr (kPairs) {
+        auto one = [](F2 x, float c1, float s1) {
+            const float2 v = split(x);
+            return kBack ? f2(v.x * c1 + v.y * s1, v.y * c1 - v.x * s1) : f2(v.x * c1 - v.y * s1, v.y * c1 + v.x * s1);
+        };
+#pragma unroll
+        for (int i = 0; i < kN / 4; ++i) {
+            const float2 ca = split(c[i]), sa = split(s[i]), cb = split(c[kN / 4 + i]), sb = split(s[kN / 4 + i]);
+            a[2 * i] = one(a[2 * i], ca.x, sa.x);
+            a[2 * i + 1] = one(a[2 * i + 1], ca.y, sa.y);
+            b[2 * i] = one(b[2 * i], cb.x, sb.x);
+            b[2 * i + 1] = one(b[2 * i + 1], cb.y, sb.y);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const float c = cs[i].x, s = sign * cs[i].y, x = a[i], y = b[i];
-            a[i] = x * c - y * s;
-            b[i] = y * c + x * s;
+        for (int i = 0; i < kN / 2; ++i) {
+            const F2 x = a[i], y = b[i];
+            a[i] = fma2(kBack ? y : negated(y), s[i], mul(x, c[i]));
+            b[i] = fma2(kBack ? negated(x) : x, s[i], mul(y, c[i]));
         }
     }
 }
@@ -114,90 +175,108 @@ __device__ __forceinline__ float sum_lanes(float x) {
     return x;
 }
 
-// The rows that a warp takes one after the other: kRows heads at a time of the units of (token, some of its heads) that are its share.
+__device__ __forceinline__ void fetch16(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+
+// The rows that a warp takes one after the other: some heads at a time of the units of (token, some of its heads) that are its share.
 struct RopeWalk {
-    int64_t token;
-    int part, h, end;      // the unit's place among its token's, the next head, the first behind the unit
-    __device__ __forceinline__ bool valid(const RopeParams& p) const { return token < p.tokens; }
+    int token, part, h, end;      // the unit's place among its token's, the next head, the first behind the unit
     __device__ __forceinline__ void enter(const RopeSide& s) {
         h = part * s.heads_per_unit;
         end = min(h + s.heads_per_unit, s.heads);
     }
-    __device__ __forceinline__ void start(const RopeSide& s, int64_t unit) {
-        token = unit / s.units_per_token;
-        part = static_cast<int>(unit - token * s.units_per_token);
-        enter(s);
-    }
-    // The next unit is step_tokens tokens and step_parts parts on.
-    __device__ __forceinline__ void next_unit(const RopeSide& s, int64_t step_tokens, int step_parts) {
-        token += step_tokens;
-        part += step_parts;
+    __device__ __forceinline__ void next_unit(const RopeSide& s) {
+        token += s.step_tokens;
+        part += s.step_parts;
         if (part >= s.units_per_token) { part -= s.units_per_token; ++token; }
         enter(s);
     }
 };
 
-__device__ __forceinline__ void fetch16(uint32_t to, const void* from) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-
 // kLanes lanes to a row (the power of two from the row's pieces / 2 on), 32 / kLanes rows of a warp at a time.  Each lane keeps the
 // pieces of its next kStages - 1 rows on the way into its own places of shared memory, across units: what a warp waits for was asked for rows
-// ago, and nothing is exchanged between lanes but the sums.
-template <bool kBwd> constexpr int kRopeStages = kBwd ? 4 : 6;
+// ago, and nothing is exchanged between lanes but the sums and the angles.  Few rows ahead are enough, and more cost time (16384 x 40 heads of 128: forward
+// 59.5 us with 3 stages, 62.2 with 5, 62.8 with 8; backward 84 with 2, 92 with 3, 94 with 4).
+template <bool kBwd> constexpr int kRopeStages = kBwd ? 2 : 3;
 template <bool kBwd> constexpr int kRopePieces = kBwd ? 4 : 2;      // 16-byte pieces of a lane for a row: two of x, two of the gradient
 template <bool kBwd> constexpr int kRopeRing = kRopeWarps * kRopeStages<kBwd> * kRopePieces<kBwd> * 32 * 16;
+// Behind them, for each warp, the cosines of a token's pairs and those of what is not turned, then the sines.
+constexpr int kStill = 8;
+__host__ __device__ constexpr int rope_angles(int half) { return half + kStill; }
 
 template <typename T, int kLanes, bool kPairs, bool kBwd>
-__global__ void __launch_bounds__(kRopeThreads, kBwd ? 2 : 3) rope_kernel(const RopeParams p) {
-    constexpr int kN = Piece<T>::kN, kRows = 32 / kLanes, kStages = kRopeStages<kBwd>, kPieces = kRopePieces<kBwd>;
-    extern __shared__ __align__(16) unsigned char rope_smem[];      // the lanes' pieces, then each warp's angles
+__global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams p) {
+    constexpr int kN = Piece<T>::kN, kRows = 32 / kLanes, kStages = kRopeStages<kBwd>, kPieces = kRopePieces<kBwd>, kStage = kPieces * 32 * 16;
+    constexpr bool kExact = sizeof(T) == 4;
+    static_assert(kStill >= kN, "");
+    extern __shared__ __align__(16) unsigned char rope_smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bool key = static_cast<int>(blockIdx.x) >= p.side[0].blocks;
     const RopeSide& s = p.side[key ? 1 : 0];
     const int block = static_cast<int>(blockIdx.x) - (key ? p.side[0].blocks : 0);
     // this lane's pieces: the first ones of a row cover the pairs, the others what is not turned
-    const int l = lane % kLanes, row = lane / kLanes, half = p.rot / 2;
+    const int l = lane % kLanes, row = lane / kLanes, half = p.rot / 2, tokens = static_cast<int>(p.tokens);
     const bool there = 2 * kN * l < p.dim, turned = kN * l < half;
     const int ia = turned ? kN * l : p.rot + kN * l - half, ib = ia + (turned ? half : (p.dim - p.rot) / 2);
     unsigned char* const ring = rope_smem + (warp * kStages * kPieces * 32 + lane) * 16;
     const uint32_t ring_at = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
-    float2* const angles = reinterpret_cast<float2*>(rope_smem + kRopeRing<kBwd>) + warp * half;
-    const int64_t step = static_cast<int64_t>(s.blocks) * kRopeWarps, step_tokens = step / s.units_per_token;
-    const int step_parts = static_cast<int>(step - step_tokens * s.units_per_token);
+    float* const cosines = reinterpret_cast<float*>(rope_smem + kRopeRing<kBwd>) + warp * 2 * rope_angles(half);
+    float* const sines = cosines + rope_angles(half);
+    const int pair_a = turned ? (kPairs ? ia / 2 : ia) : half, pair_b = turned ? ib / 2 : half;      // pair_b: PF_ROPE_PAIRS only
     RopeWalk ahead, at;      // rows to ask for, rows to compute
-    ahead.start(s, static_cast<int64_t>(block) * kRopeWarps + warp);
-    at = ahead;
+    {
+        const unsigned unit = static_cast<unsigned>(block) * kRopeWarps + warp, per = static_cast<unsigned>(s.units_per_token);
+        ahead.token = static_cast<int>(unit / per);
+        ahead.part = static_cast<int>(unit - ahead.token * per);
+        ahead.enter(s);
+        at = ahead;
+    }
+    const T* const x0 = static_cast<const T*>(s.x) + row * s.sx;
+    const T* const g0 = static_cast<const T*>(s.g) + row * s.sg;
+    const T* xp = x0 + ahead.token * s.ldx + ahead.h * s.sx;
+    const T* gp = g0 + ahead.token * s.ldg + ahead.h * s.sg;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const T* const xs = static_cast<const T*>(s.x);
-    const T* const gs = static_cast<const T*>(s.g);
     auto ask = [&](int stage) {
-        if (ahead.valid(p)) {
-            const int64_t head = ahead.h + row;
-            if (there && head < ahead.end) {
-                const uint32_t to = ring_at + stage * (kPieces * 32 * 16);
-                const T* const x = xs + ahead.token * s.ldx + head * s.sx;
-                fetch16(to, x + ia);
-                fetch16(to + 512, x + ib);
+        if (ahead.token < tokens) {
+            if (there && ahead.h + row < ahead.end) {
+                const uint32_t to = ring_at + stage * kStage;
+                fetch16(to, xp + ia);
+                fetch16(to + 512, xp + ib);
                 if constexpr (kBwd) {
-                    const T* const g = gs + ahead.token * s.ldg + head * s.sg;
-                    fetch16(to + 1024, g + ia);
-                    fetch16(to + 1536, g + ib);
+                    fetch16(to + 1024, gp + ia);
+                    fetch16(to + 1536, gp + ib);
                 }
             }
             ahead.h += kRows;
-            if (ahead.h >= ahead.end) ahead.next_unit(s, step_tokens, step_parts);
+            if (ahead.h >= ahead.end) {
+                ahead.next_unit(s);
+                xp = x0 + ahead.token * s.ldx + ahead.h * s.sx;
+                if constexpr (kBwd) gp = g0 + ahead.token * s.ldg + ahead.h * s.sg;
+            } else {
+                xp += kRows * s.sx;
+                if constexpr (kBwd) gp += kRows * s.sg;
+            }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i) ask(i);
-    auto position_of = [&](const RopeWalk& w) { return !w.valid(p) ? 0 : p.positions ? p.positions[w.token] : w.token; };
+    auto position_of = [&](const RopeWalk& w) -> int64_t { return w.token >= tokens ? 0 : p.positions ? p.positions[w.token] : w.token; };
     int64_t position = position_of(at);
-    float wa[kN], wb[kN];
+    // the turns of this lane's first angles for a position (those of rows of more than 128 pairs are made again for each token)
+    constexpr int kKept = 2;
+    uint64_t each[kKept];
 #pragma unroll
-    for (int i = 0; i < kN; ++i) wa[i] = wb[i] = 1.f;
+    for (int i = 0; i < kKept; ++i) each[i] = lane + 32 * i < half ? turn_per_position(p.inv_freq[lane + 32 * i]) : 0;
+    if (lane < kStill) {
+        cosines[half + lane] = 1.f;
+        sines[half + lane] = 0.f;
+    }
+    F2 wa[kN / 2], wb[kN / 2];
+#pragma unroll
+    for (int i = 0; i < kN / 2; ++i) wa[i] = wb[i] = f2(1.f, 1.f);
     if (s.w && there) {
         Piece<T> t;
         t.load(static_cast<const T*>(s.w) + ia);
@@ -205,83 +284,96 @@ __global__ void __launch_bounds__(kRopeThreads, kBwd ? 2 : 3) rope_kernel(const 
         t.load(static_cast<const T*>(s.w) + ib);
         t.get(wb);
     }
-    float dwa[kN], dwb[kN];
+    F2 dwa[kN / 2], dwb[kN / 2];
 #pragma unroll
-    for (int i = 0; i < kN; ++i) dwa[i] = dwb[i] = 0.f;
+    for (int i = 0; i < kN / 2; ++i) dwa[i] = dwb[i] = f2(0.f, 0.f);
     const float inv_dim = 1.f / static_cast<float>(p.dim);
     int stage = 0;
-    while (at.valid(p)) {
+    while (at.token < tokens) {
         __syncwarp();
-        for (int i = lane; i < half; i += 32) angles[i] = turn_of(position, p.inv_freq[i]);
-        __syncwarp();
-        float2 cs[kN];
+        auto angle = [&](int i, uint64_t turns) {
+            const float2 v = turn_of<kExact>(position, turns);
+            cosines[i] = v.x;
+            sines[i] = v.y;
+        };
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const int pair = kPairs ? (i < kN / 2 ? ia / 2 + i : ib / 2 + i - kN / 2) : ia + i;
-            cs[i] = turned ? angles[pair] : make_float2(1.f, 0.f);
+        for (int i = 0; i < kKept; ++i)
+            if (lane + 32 * i < half) angle(lane + 32 * i, each[i]);
+        for (int i = lane + 32 * kKept; i < half; i += 32) angle(i, turn_per_position(p.inv_freq[i]));
+        __syncwarp();
+        F2 c[kN / 2], sn[kN / 2];
+#pragma unroll
+        for (int i = 0; i < kN / 2; ++i) {
+            const int at_pair = !kPairs ? pair_a + 2 * i : i < kN / 4 ? pair_a + 2 * i : pair_b + 2 * i - kN / 2;
+            c[i] = *reinterpret_cast<const F2*>(cosines + at_pair);
+            sn[i] = *reinterpret_cast<const F2*>(sines + at_pair);
         }
         RopeWalk next = at;
-        next.next_unit(s, step_tokens, step_parts);
+        next.next_unit(s);
         position = position_of(next);
-        T* const out = static_cast<T*>(s.out) + at.token * s.ldo;
-        for (; at.h < at.end; at.h += kRows) {
+        T* out = static_cast<T*>(s.out) + at.token * s.ldo + (at.h + row) * s.so;
+        for (; at.h < at.end; at.h += kRows, out += kRows * s.so) {
             __syncwarp();
             ask(stage == 0 ? kStages - 1 : stage - 1);      // the place that the row before has left
             asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-            const unsigned char* const in = ring + stage * (kPieces * 32 * 16);
+            const unsigned char* const in = ring + stage * kStage;
             stage = stage == kStages - 1 ? 0 : stage + 1;
-            const int64_t head = at.h + row;
-            const bool live = head < at.end, on = there && live;
-            float a[kN], b[kN];
+            const bool live = at.h + row < at.end, on = there && live;
+            F2 a[kN / 2], b[kN / 2];
             Piece<T> xa, xb;
             xa.raw = {};
             xb.raw = {};
             if (on) {
-                xa.load(reinterpret_cast<const T*>(in));
-                xb.load(reinterpret_cast<const T*>(in + 512));
+                xa.load(in);
+                xb.load(in + 512);
             }
             xa.get(a);
             xb.get(b);
-            float sq = 0.f;
+            F2 sq2 = mul(a[0], a[0]);
 #pragma unroll
-            for (int i = 0; i < kN; ++i) sq = fmaf(a[i], a[i], fmaf(b[i], b[i], sq));
-            sq = sum_lanes<kLanes>(sq);
+            for (int i = 1; i < kN / 2; ++i) sq2 = fma2(a[i], a[i], sq2);
+#pragma unroll
+            for (int i = 0; i < kN / 2; ++i) sq2 = fma2(b[i], b[i], sq2);
+            const float2 pairs2 = split(sq2);
+            const float sq = sum_lanes<kLanes>(pairs2.x + pairs2.y);      // (all lanes take part)
             // (a row behind the last head adds nothing to dw, whatever eps is)
             const float r = live ? rsqrtf(fmaf(sq, inv_dim, p.eps)) : 0.f;
+            const F2 rr = f2(r, r);
             if constexpr (!kBwd) {
 #pragma unroll
-                for (int i = 0; i < kN; ++i) { a[i] *= r * wa[i]; b[i] *= r * wb[i]; }
-                turn<kN, kPairs>(a, b, cs, 1.f);
+                for (int i = 0; i < kN / 2; ++i) { a[i] = mul(a[i], mul(rr, wa[i])); b[i] = mul(b[i], mul(rr, wb[i])); }
+                turn<kN, kPairs, false>(a, b, c, sn);
             } else {
-                Piece<T> ga, gb;
-                ga.raw = {};
-                gb.raw = {};
+                F2 ea[kN / 2], eb[kN / 2];
+                xa.raw = {};
+                xb.raw = {};
                 if (on) {
-                    ga.load(reinterpret_cast<const T*>(in + 1024));
-                    gb.load(reinterpret_cast<const T*>(in + 1536));
+                    xa.load(in + 1024);
+                    xb.load(in + 1536);
                 }
-                float ea[kN], eb[kN], dot = 0.f;
-                ga.get(ea);
-                gb.get(eb);
-                turn<kN, kPairs>(ea, eb, cs, -1.f);
+                xa.get(ea);
+                xb.get(eb);
+                turn<kN, kPairs, true>(ea, eb, c, sn);
+                F2 dot2 = f2(0.f, 0.f);
 #pragma unroll
-                for (int i = 0; i < kN; ++i) {
-                    a[i] *= r;
-                    b[i] *= r;
-                    dwa[i] = fmaf(ea[i], a[i], dwa[i]);
-                    dwb[i] = fmaf(eb[i], b[i], dwb[i]);
-                    ea[i] *= wa[i];
-                    eb[i] *= wb[i];
-                    dot = fmaf(ea[i], a[i], fmaf(eb[i], b[i], dot));
+                for (int i = 0; i < kN / 2; ++i) {
+                    a[i] = mul(a[i], rr);
+                    b[i] = mul(b[i], rr);
+                    dwa[i] = fma2(ea[i], a[i], dwa[i]);
+                    dwb[i] = fma2(eb[i], b[i], dwb[i]);
+                    ea[i] = mul(ea[i], wa[i]);
+                    eb[i] = mul(eb[i], wb[i]);
+                    dot2 = fma2(ea[i], a[i], fma2(eb[i], b[i], dot2));
                 }
-                dot = sum_lanes<kLanes>(dot) * inv_dim;
+                const float2 d = split(dot2);
+                const float dot = -sum_lanes<kLanes>(d.x + d.y) * inv_dim;
+                const F2 dd = f2(dot, dot);
 #pragma unroll
-                for (int i = 0; i < kN; ++i) { a[i] = r * (ea[i] - a[i] * dot); b[i] = r * (eb[i] - b[i] * dot); }
+                for (int i = 0; i < kN / 2; ++i) { a[i] = mul(rr, fma2(a[i], dd, ea[i])); b[i] = mul(rr, fma2(b[i], dd, eb[i])); }
             }
             if (on) {
-                T* const o = out + head * s.so;
-                Piece<T>::store(o + ia, a);
-                Piece<T>::store(o + ib, b);
+                Piece<T>::store(out + ia, a);
+                Piece<T>::store(out + ib, b);
             }
         }
         at = next;
@@ -295,25 +387,26 @@ __global__ void __launch_bounds__(kRopeThreads, kBwd ? 2 : 3) rope_kernel(const 
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
+            float da = i % 2 ? split(dwa[i / 2]).y : split(dwa[i / 2]).x, db = i % 2 ? split(dwb[i / 2]).y : split(dwb[i / 2]).x;
 #pragma unroll
             for (int o = kLanes; o < 32; o *= 2) {
-                dwa[i] += __shfl_xor_sync(0xffffffffu, dwa[i], o);
-                dwb[i] += __shfl_xor_sync(0xffffffffu, dwb[i], o);
+                da += __shfl_xor_sync(0xffffffffu, da, o);
+                db += __shfl_xor_sync(0xffffffffu, db, o);
             }
             if (row == 0) {
-                red[(warp * 2 * kN + i) * kLanes + l] = dwa[i];
-                red[(warp * 2 * kN + kN + i) * kLanes + l] = dwb[i];
+                red[(warp * 2 * kN + i) * kLanes + l] = da;
+                red[(warp * 2 * kN + kN + i) * kLanes + l] = db;
             }
         }
         __syncthreads();
-        for (int c = threadIdx.x; c < 2 * kN * kLanes; c += kRopeThreads) {
-            const int cl = c % kLanes, i = c / kLanes;
+        for (int i = threadIdx.x; i < 2 * kN * kLanes; i += kRopeThreads) {
+            const int cl = i % kLanes, e = i / kLanes;
             if (2 * kN * cl >= p.dim) continue;
             float sum = 0.f;
-            for (int w = 0; w < kRopeWarps; ++w) sum += red[(w * 2 * kN + i) * kLanes + cl];
+            for (int w = 0; w < kRopeWarps; ++w) sum += red[(w * 2 * kN + e) * kLanes + cl];
             const bool t = kN * cl < half;
             const int a0 = t ? kN * cl : p.rot + kN * cl - half, b0 = a0 + (t ? half : (p.dim - p.rot) / 2);
-            s.partial[static_cast<int64_t>(block) * p.dim + (i < kN ? a0 + i : b0 + i - kN)] = sum;
+            s.partial[static_cast<int64_t>(block) * p.dim + (e < kN ? a0 + e : b0 + e - kN)] = sum;
         }
     }
 }
@@ -343,7 +436,7 @@ __global__ void __launch_bounds__(kAnyThreads) rope_any_kernel(const RopeParams 
         const int head1 = min(head0 + s.heads_per_unit, s.heads);
         const int64_t position = p.positions ? p.positions[token] : token;
         __syncwarp();
-        for (int i = lane; i < half; i += 32) cs[i] = turn_of(position, p.inv_freq[i]);
+        for (int i = lane; i < half; i += 32) cs[i] = turn_of<true>(position, turn_per_position(p.inv_freq[i]));
         __syncwarp();
         for (int64_t head = head0; head < head1; ++head) {
             const T* const x = static_cast<const T*>(s.x) + token * s.ldx + head * s.sx;
@@ -441,10 +534,21 @@ struct RopePlan {
     bool pieces;
     int lanes, warps;            // lanes of a row, warps of a block
     int blocks[2], heads_per_unit[2], units_per_token[2];
+    RopeSide side(int i, RopeSide s) const {
+        s.heads_per_unit = heads_per_unit[i];
+        s.units_per_token = units_per_token[i];
+        s.blocks = blocks[i];
+        if (s.heads > 0) {
+            s.step_tokens = blocks[i] * warps / units_per_token[i];
+            s.step_parts = blocks[i] * warps % units_per_token[i];
+        }
+        return s;
+    }
 };
-// Blocks of an SM: what its shared memory holds of the vector kernels (64 and 80 KB each with the most angles), and as many of the others.
-constexpr int rope_blocks_per_sm(bool bwd) { return bwd ? 2 : 3; }
-RopePlan rope_plan(int64_t tokens, const int (&heads)[2], int dim, int rot, int dtype, bool pieces, bool bwd) {
+// Blocks of an SM: two of the vector kernels, whose registers (80 for three forward ones) would otherwise spill: 16384 x 40 heads of 128 forward 66 us with
+// three, 59.5 with two.  Twice as many of the others.
+constexpr int kRopeBlocksPerSm = 2;
+RopePlan rope_plan(int64_t tokens, const int (&heads)[2], int dim, int rot, int dtype, bool pieces) {
     RopePlan pl = {};
     const int n = 16 / static_cast<int>(dtype_size(dtype));
     pl.pieces = pieces && dim % (2 * n) == 0 && rot % (2 * n) == 0 && dim / (2 * n) <= 32 && rot / 2 <= kMaxPairs;
@@ -452,17 +556,25 @@ RopePlan rope_plan(int64_t tokens, const int (&heads)[2], int dim, int rot, int 
     if (pl.pieces)
         for (pl.lanes = 2; pl.lanes < dim / (2 * n);) pl.lanes *= 2;
     pl.warps = pl.pieces ? kRopeWarps : kAnyWarps;
-    const int rows = pl.pieces ? 32 / pl.lanes : 1, all = heads[0] + heads[1];
-    const int64_t most = static_cast<int64_t>(num_sms()) * rope_blocks_per_sm(bwd) * (pl.pieces ? 1 : 2);
+    const int rows = pl.pieces ? 32 / pl.lanes : 1;
+    const int64_t most = static_cast<int64_t>(num_sms()) * kRopeBlocksPerSm * (pl.pieces ? 1 : 2);
+    // Blocks by the time that a side takes: a warp's turn at some heads, and what a unit costs besides, kUnit of one.
+    constexpr double kUnit = 0.5;
+    int64_t turns[2] = {ceil_div(heads[0], rows), ceil_div(heads[1], rows)};      // of a token
+    const double q = turns[0] ? turns[0] + kUnit : 0, k = turns[1] ? turns[1] + kUnit : 0;
     for (int i = 0; i < 2; ++i) {
         if (heads[i] == 0) continue;
-        // all heads of a token in one unit, unless that leaves warps without any
-        const int64_t wanted = ceil_div(most * pl.warps, tokens);
-        const int per_warp = static_cast<int>(ceil_div(heads[i], rows));
-        const int units = static_cast<int>(std::min<int64_t>(per_warp, std::max<int64_t>(1, wanted * heads[i] / all)));
-        pl.heads_per_unit[i] = static_cast<int>(ceil_div(per_warp, units)) * rows;
+        const int64_t share = std::max<int64_t>(1, static_cast<int64_t>(most * (i ? k : q) / (q + k)));
+        // units as large as leave the warps equal shares
+        double best = 0;
+        for (int64_t units = 1; units <= turns[i]; units *= 2) {
+            const int64_t each = ceil_div(turns[i], units);
+            const double time = static_cast<double>(ceil_div(tokens * ceil_div(turns[i], each), share * pl.warps)) * (each + kUnit);
+            if (units > 1 && time > 0.98 * best) continue;
+            best = time;
+            pl.heads_per_unit[i] = static_cast<int>(each) * rows;
+        }
         pl.units_per_token[i] = static_cast<int>(ceil_div(heads[i], pl.heads_per_unit[i]));
-        const int64_t share = std::max<int64_t>(1, most * heads[i] / all);
         pl.blocks[i] = static_cast<int>(std::min<int64_t>(share, ceil_div(tokens * pl.units_per_token[i], pl.warps)));
     }
     return pl;
@@ -472,9 +584,9 @@ template <typename T, int kLanes, bool kPairs, bool kBwd>
 cudaError_t rope_styled(const RopeParams& p, int blocks, cudaStream_t stream) {
     static std::atomic<uint64_t> allowed{0};
     const auto kernel = rope_kernel<T, kLanes, kPairs, kBwd>;
-    const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), kRopeRing<kBwd> + kRopeWarps * kMaxPairs * sizeof(float2), allowed);
+    const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), kRopeRing<kBwd> + kRopeWarps * rope_angles(kMaxPairs) * sizeof(float2), allowed);
     if (e != cudaSuccess) return e;
-    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kRopeThreads, kRopeRing<kBwd> + kRopeWarps * (p.rot / 2) * sizeof(float2), 1, stream, p);
+    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kRopeThreads, kRopeRing<kBwd> + kRopeWarps * rope_angles(p.rot / 2) * sizeof(float2), 1, stream, p);
 }
 template <typename T, int kLanes, bool kBwd>
 cudaError_t rope_pieces(const RopeParams& p, bool pairs, int blocks, cudaStream_t stream) {
@@ -508,7 +620,7 @@ int validate_rope(const RowsView (&x)[2], const void* const (&w)[2], const int64
         if (heads[i] > 0 && tokens > 0 && (!rows_valid(x[i], tokens, heads[i], dim, dtype) || !rows_valid(out[i], tokens, heads[i], dim, dtype)))
             return PF_ERR_INVALID_ARG;
     }
-    if (dim > kMaxDim || tokens > (1LL << 31) || heads[0] > (1 << 16) || heads[1] > (1 << 16)) return PF_ERR_UNSUPPORTED;
+    if (dim > kMaxDim || tokens > (1LL << 30) || heads[0] > (1 << 16) || heads[1] > (1 << 16)) return PF_ERR_UNSUPPORTED;
     return PF_OK;
 }
 
@@ -532,7 +644,7 @@ int pf_qk_norm_rope_fwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
     for (int i = 0; i < 2; ++i)
         if (heads[i] > 0)
             pieces = pieces && rows_in_pieces(x[i], dtype) && rows_in_pieces(out[i], dtype) && reinterpret_cast<uintptr_t>(w[i]) % 16 == 0;
-    const RopePlan pl = rope_plan(tokens, heads, dim, rot_dim, dtype, pieces, false);
+    const RopePlan pl = rope_plan(tokens, heads, dim, rot_dim, dtype, pieces);
     RopeParams p = {};
     p.positions = positions;
     p.inv_freq = inv_freq;
@@ -541,8 +653,7 @@ int pf_qk_norm_rope_fwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
     p.rot = rot_dim;
     p.eps = static_cast<float>(eps);
     for (int i = 0; i < 2; ++i)
-        p.side[i] = RopeSide{x[i].p, w[i], nullptr, const_cast<void*>(out[i].p), nullptr, x[i].ld, x[i].s, 0, 0, out[i].ld, out[i].s, heads[i],
-                             pl.heads_per_unit[i], pl.units_per_token[i], pl.blocks[i]};
+        p.side[i] = pl.side(i, RopeSide{x[i].p, w[i], nullptr, const_cast<void*>(out[i].p), nullptr, x[i].ld, x[i].s, 0, 0, out[i].ld, out[i].s, heads[i]});
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool pairs = style == PF_ROPE_PAIRS;
     PF_CUDA((dtype == PF_BF16 ? rope_launch<__nv_bfloat16, false>(p, pl, pairs, stream) : rope_launch<float, false>(p, pl, pairs, stream)));
@@ -552,7 +663,7 @@ int pf_qk_norm_rope_fwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
 size_t pf_qk_norm_rope_bwd_workspace(int64_t tokens, int q_heads, int k_heads, int dim) {
     if (tokens <= 0 || q_heads < 0 || k_heads < 0 || dim < 1) return 0;
     // a row of sums for each block, of which there are at most so many on either side
-    return align_up(sizeof(float) * dim * (static_cast<size_t>(num_sms()) * 2 * rope_blocks_per_sm(true) + 2), 256);
+    return align_up(sizeof(float) * dim * (static_cast<size_t>(num_sms()) * 2 * kRopeBlocksPerSm + 2), 256);
 }
 
 int pf_qk_norm_rope_bwd(const void* q, int64_t ldq, int64_t sq, const void* k, int64_t ldk, int64_t sk, const void* wq, const void* wk,
@@ -585,7 +696,7 @@ int pf_qk_norm_rope_bwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
             if (dw[i] && !(flags & PF_GRAD_ACCUMULATE)) PF_CUDA(cudaMemsetAsync(dw[i], 0, dim * dtype_size(wtype), stream));
         return PF_OK;
     }
-    const RopePlan pl = rope_plan(tokens, heads, dim, rot_dim, dtype, pieces, true);
+    const RopePlan pl = rope_plan(tokens, heads, dim, rot_dim, dtype, pieces);
     RopeParams p = {};
     p.positions = positions;
     p.inv_freq = inv_freq;
@@ -597,8 +708,7 @@ int pf_qk_norm_rope_bwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
     WeightSums ws = {};
     for (int i = 0; i < 2; ++i) {
         float* const part = dw[i] ? partial + static_cast<int64_t>(i ? pl.blocks[0] : 0) * dim : nullptr;
-        p.side[i] = RopeSide{x[i].p, w[i], g[i].p, const_cast<void*>(out[i].p), part, x[i].ld, x[i].s, g[i].ld, g[i].s, out[i].ld, out[i].s, heads[i],
-                             pl.heads_per_unit[i], pl.units_per_token[i], pl.blocks[i]};
+        p.side[i] = pl.side(i, RopeSide{x[i].p, w[i], g[i].p, const_cast<void*>(out[i].p), part, x[i].ld, x[i].s, g[i].ld, g[i].s, out[i].ld, out[i].s, heads[i]});
         ws.partial[i] = part;
         ws.out[i] = dw[i];
         ws.blocks[i] = pl.blocks[i];
