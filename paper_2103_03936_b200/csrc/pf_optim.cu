@@ -21,6 +21,7 @@
 
 #include <cmath>
 
+#include "pf_f32x2.cuh"
 #include "pf_internal.h"
 
 namespace pf {
@@ -58,20 +59,38 @@ struct AdamHyper {
     const pf_adamw_scalars* scalars;   // replace lr, r1, r2, grad_scale and seed
 };
 
+// (Operands below the normal numbers count as zero: eps is at least 2^-63, the root of the smallest normal number.)
 __device__ __forceinline__ float sqrt_fast(float x) {
     float y;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-
-__device__ __forceinline__ void moments(const AdamHyper& h, float grad, float& m, float& v) {
-    const float g = __fmul_rn(grad, h.grad_scale);
-    m = __fadd_rn(__fmul_rn(m, h.b1), __fmul_rn(g, h.c1));
-    v = __fadd_rn(__fmul_rn(v, h.b2), __fmul_rn(__fmul_rn(g, g), h.c2));
+__device__ __forceinline__ float rcp_fast(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-__device__ __forceinline__ float stepped(const AdamHyper& h, float p, float m, float v) {
-    const float u = __fdividef(m * h.r1, sqrt_fast(v * h.r2) + h.eps);
-    return fmaf(-h.lr, fmaf(h.wd, p, u), p);
+__device__ __forceinline__ F2 both(float x) { return f2(x, x); }
+
+// The hyperparameters as pairs of fp32 numbers.
+struct AdamPairs {
+    F2 b1, c1, b2, c2, eps, wd, minus_lr, r1, r2, grad_scale;
+    __device__ __forceinline__ explicit AdamPairs(const AdamHyper& h)
+        : b1(both(h.b1)), c1(both(h.c1)), b2(both(h.b2)), c2(both(h.c2)), eps(both(h.eps)), wd(both(h.wd)), minus_lr(both(-h.lr)), r1(both(h.r1)),
+          r2(both(h.r2)), grad_scale(both(h.grad_scale)) {}
+};
+// m and v of two elements after the step; b1m = beta1 times a power of two where m is in units of that (and b2v).
+__device__ __forceinline__ void moments(const AdamPairs& h, F2 grad, F2 b1m, F2 b2v, F2& m, F2& v) {
+    // (A product that is a fused multiply-add with zero is rounded by itself: one that is added as it is gets fused with the sum in the end.)
+    const F2 zero = both(0.f), g = mul2(grad, h.grad_scale);
+    m = add2(fma2(m, b1m, zero), fma2(g, h.c1, zero));
+    v = add2(fma2(v, b2v, zero), fma2(mul2(g, g), h.c2, zero));
+}
+__device__ __forceinline__ F2 stepped(const AdamPairs& h, F2 p, F2 m, F2 v) {
+    const float2 w = split(mul2(v, h.r2));
+    const float2 d = split(add2(f2(sqrt_fast(w.x), sqrt_fast(w.y)), h.eps));
+    const F2 u = mul2(mul2(m, h.r1), f2(rcp_fast(d.x), rcp_fast(d.y)));
+    return fma2(h.minus_lr, fma2(h.wd, p, u), p);
 }
 
 __device__ __forceinline__ float bf16_to_f32(unsigned short raw) { return __uint_as_float(static_cast<unsigned>(raw) << 16); }
@@ -79,24 +98,36 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
     const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const unsigned*>(&t);
 }
-// Eight elements at a 16-byte boundary (bf16) or two (fp32).
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
-    const unsigned w[4] = {a.x, a.y, a.z, a.w};
+// Eight elements at a 16-byte boundary, as they lie in memory.
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); b = *reinterpret_cast<const float4*>(p + 4); }
+    __device__ __forceinline__ void get(F2 (&x)[4]) const { x[0] = f2(a.x, a.y); x[1] = f2(a.z, a.w); x[2] = f2(b.x, b.y); x[3] = f2(b.z, b.w); }
+    static __device__ __forceinline__ void store(float* p, const F2 (&x)[4]) {
+        const float2 c = split(x[0]), d = split(x[1]), e = split(x[2]), f = split(x[3]);
+        *reinterpret_cast<float4*>(p) = make_float4(c.x, c.y, d.x, d.y);
+        *reinterpret_cast<float4*>(p + 4) = make_float4(e.x, e.y, f.x, f.y);
+    }
+};
+template <> struct Eight<__nv_bfloat16> {
+    uint4 a;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { a = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void get(F2 (&x)[4]) const {
+        const unsigned w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-}
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-    *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-}
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-}
+        for (int i = 0; i < 4; ++i) x[i] = f2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    }
+    static __device__ __forceinline__ void store(__nv_bfloat16* p, const F2 (&x)[4]) {
+        unsigned w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = split(x[i]);
+            w[i] = pack_bf16(f.x, f.y);
+        }
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 __device__ __forceinline__ float load1(const __nv_bfloat16* p) { return bf16_to_f32(*reinterpret_cast<const unsigned short*>(p)); }
 __device__ __forceinline__ void store1(float* p, float x) { *p = x; }
@@ -105,21 +136,21 @@ __device__ __forceinline__ void store1(__nv_bfloat16* p, float x) { *p = __float
 template <int kParam> struct ParamType { using T = __nv_bfloat16; };
 template <> struct ParamType<P_F32> { using T = float; };
 
-// The arrays of one tensor.
+// What a step reads of the parameters, and the arrays of one tensor.
+template <int kParam> struct ReadType { using T = typename ParamType<kParam>::T; };
+template <> struct ReadType<P_MASTER> { using T = float; };
 template <int kParam, typename G>
 struct Arrays {
+    using R = typename ReadType<kParam>::T;
     typename ParamType<kParam>::T* p;
     float* master;
     const G* g;
-    __device__ __forceinline__ void load8p(int64_t i, float (&x)[8]) const {
-        if constexpr (kParam == P_MASTER) load8(master + i, x); else load8(p + i, x);
+    __device__ __forceinline__ const R* read() const {
+        if constexpr (kParam == P_MASTER) return master; else return p;
     }
-    __device__ __forceinline__ void store8p(int64_t i, const float (&x)[8]) const {
-        if constexpr (kParam == P_MASTER) store8(master + i, x);
-        store8(p + i, x);
-    }
-    __device__ __forceinline__ float load1p(int64_t i) const {
-        if constexpr (kParam == P_MASTER) return master[i]; else return load1(p + i);
+    __device__ __forceinline__ void store8p(int64_t i, const F2 (&x)[4]) const {
+        if constexpr (kParam == P_MASTER) Eight<float>::store(master + i, x);
+        Eight<typename ParamType<kParam>::T>::store(p + i, x);
     }
     __device__ __forceinline__ void store1p(int64_t i, float x) const {
         if constexpr (kParam == P_MASTER) master[i] = x;
@@ -161,13 +192,14 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     float* const ms = static_cast<float*>(tb.m[t]);
     float* const vs = static_cast<float*>(tb.v[t]);
     const int64_t n = tb.n[t];
+    const AdamPairs hp(h);
     auto single = [&](int64_t i) {
-        float m = ms[i], v = vs[i];
-        const float p = a.load1p(i);
-        moments(h, load1(a.g + i), m, v);
-        ms[i] = m;
-        vs[i] = v;
-        a.store1p(i, stepped(h, p, m, v));
+        F2 m = f2(ms[i], 0.f), v = f2(vs[i], 0.f);
+        const F2 p = f2(load1(a.read() + i), 0.f);
+        moments(hp, f2(load1(a.g + i), 0.f), hp.b1, hp.b2, m, v);
+        ms[i] = split(m).x;
+        vs[i] = split(v).x;
+        a.store1p(i, split(stepped(hp, p, m, v)).x);
     };
     const int head = tb.head[t];
     if (head == kNoVectors) {
@@ -183,144 +215,197 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
         if (i < n) single(i);
     }
     const int64_t first = static_cast<int64_t>(local) * (kAdamThreads * kAdamDeep) + threadIdx.x;
-    float g[kAdamDeep][8], m[kAdamDeep][8], v[kAdamDeep][8], p[kAdamDeep][8];
+    Eight<G> g[kAdamDeep];
+    Eight<float> m[kAdamDeep], v[kAdamDeep];
+    Eight<typename Arrays<kParam, G>::R> p[kAdamDeep];
 #pragma unroll
     for (int u = 0; u < kAdamDeep; ++u) {
         const int64_t k = first + u * kAdamThreads, i = head + k * kAdamVec;
-        if (k < vectors) { load8(a.g + i, g[u]); load8(ms + i, m[u]); load8(vs + i, v[u]); a.load8p(i, p[u]); }
+        if (k < vectors) { g[u].load(a.g + i); m[u].load(ms + i); v[u].load(vs + i); p[u].load(a.read() + i); }
     }
 #pragma unroll
     for (int u = 0; u < kAdamDeep; ++u) {
         const int64_t k = first + u * kAdamThreads, i = head + k * kAdamVec;
         if (k >= vectors) break;
+        F2 fg[4], fm[4], fv[4], fp[4];
+        g[u].get(fg);
+        m[u].get(fm);
+        v[u].get(fv);
+        p[u].get(fp);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            moments(h, g[u][e], m[u][e], v[u][e]);
-            p[u][e] = stepped(h, p[u][e], m[u][e], v[u][e]);
+        for (int e = 0; e < 4; ++e) {
+            moments(hp, fg[e], hp.b1, hp.b2, fm[e], fv[e]);
+            fp[e] = stepped(hp, fp[e], fm[e], fv[e]);
         }
-        store8(ms + i, m[u]);
-        store8(vs + i, v[u]);
-        a.store8p(i, p[u]);
+        Eight<float>::store(ms + i, fm);
+        Eight<float>::store(vs + i, fv);
+        a.store8p(i, fp);
     }
 }
 
 // ------------------------------------------------------------------------------ 8-bit states
 // 32 random bits for an element: a key for the tensor and the seed, then two rounds of multiply and fold.
 __device__ __forceinline__ uint32_t tensor_key(uint32_t seed, int tensor) { return seed + static_cast<uint32_t>(tensor + 1) * 0x9E3779B9u; }
-__device__ __forceinline__ uint32_t random_bits(uint32_t key, uint32_t index) {
-    uint32_t x = (index ^ key) * 0xA3D95FA7u;
-    x ^= x >> 15;
-    x *= 0xC8B1F265u;
-    return x ^ (x >> 16);
-}
+constexpr uint32_t kFirstRound = 0xA3D95FA7u, kSecondRound = 0xC8B1F265u, kBeyond32 = 0x9C2F1D35u;
+// `x`: (the element's place ^ key) * kFirstRound.  Returns the bits before the last fold, whose upper half is v's and whose halves together are m's.
+__device__ __forceinline__ uint32_t random_bits(uint32_t x) { return (x ^ (x >> 15)) * kSecondRound; }
 
-// The two formats: kCut fp32 mantissa bits that are cut off, kBias the exponent bias, kTop the binade of a block's largest value,
-// kLeast the least exponent field of a scale (so that fp32 numbers below the normal ones are below the format's as well).
-struct E4M3 { static constexpr int kCut = 20, kBias = 7, kTop = 7, kLeast = 8; };
-struct E5M2 { static constexpr int kCut = 21, kBias = 15, kTop = 14, kLeast = 16; };
+// The two formats: kCut fp32 mantissa bits that are cut off, kTop the binade of a block's largest value, kLeast the least exponent
+// field of a scale (so that fp32 numbers below the normal ones are below the format's as well).
+struct E4M3 { static constexpr int kCut = 20, kTop = 7, kLeast = 8; };
+struct E5M2 { static constexpr int kCut = 21, kTop = 14, kLeast = 16; };
 
+// The exponent field of a block's scale, as in fp32.
 template <typename F>
 __device__ __forceinline__ int scale_field(uint32_t largest) {
     const int e = static_cast<int>(largest >> 23) - F::kTop;
     return e > F::kLeast ? e : F::kLeast;
 }
-// The code of a value's magnitude: its bits with the exponent moved by the scale, random bits added below the cut, the rest taken.
-template <typename F, bool kKeep>
-__device__ __forceinline__ uint32_t coded(uint32_t magnitude, uint32_t random16, int field) {
-    const int s = static_cast<int>(magnitude + (random16 << (F::kCut - 16)) - (static_cast<uint32_t>(field - F::kBias) << 23));
-    constexpr int kNormal = 1 << 23;
-    if (s < kNormal) return kKeep && magnitude != 0 ? static_cast<uint32_t>(kNormal >> F::kCut) : 0u;
-    return static_cast<uint32_t>(s) >> F::kCut;
+// A value with 16 random bits added below the cut and the rest cut off: rounded to the format's digits, the sign with them.
+template <typename F>
+__device__ __forceinline__ uint32_t rounded(uint32_t bits, uint32_t random16) {
+    return (bits + random16 * (1u << (F::kCut - 16))) & ~((1u << F::kCut) - 1u);
 }
 
 template <__nv_fp8_interpretation_t kFormat>
-__device__ __forceinline__ void decode4(uint32_t four, float scale, float* x) {
+__device__ __forceinline__ void decode4(uint32_t four, F2* x) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(four >> (16 * i)), kFormat);
         const float2 f = __half22float2(__half2(h));
-        x[2 * i] = f.x * scale;
-        x[2 * i + 1] = f.y * scale;
+        x[i] = f2(f.x, f.y);
     }
+}
+template <__nv_fp8_interpretation_t kFormat>
+__device__ __forceinline__ uint32_t encode4(F2 a, F2 b) {
+    return static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(split(a), __NV_SATFINITE, kFormat)) |
+           static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(split(b), __NV_SATFINITE, kFormat)) << 16;
+}
+// The larger magnitude, NaN if either is.
+__device__ __forceinline__ float larger(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
 }
 
 // A block of 256 elements of a warp: lane l has elements 8 l .. 8 l + 7 (kVectors), or l, l + 32, ... of which `left` exist.
 template <int kParam, typename G, bool kVectors>
 struct StateBlock {
-    float g[8], p[8];
+    using A = Arrays<kParam, G>;
+    Eight<G> g;
+    Eight<typename A::R> p;
+    F2 g1[kVectors ? 1 : 4], p1[kVectors ? 1 : 4];
     uint32_t m[2], v[2];
     float m_scale, v_scale;
 
     static __device__ __forceinline__ int place(int lane, int e) { return kVectors ? lane * 8 + e : e * 32 + lane; }
-    __device__ __forceinline__ void load(const Arrays<kParam, G>& a, const uint8_t* mc, const uint8_t* vc, const float* msc, const float* vsc,
-                                         int64_t beg, int left, int lane) {
+    __device__ __forceinline__ void load(const A& a, const uint8_t* mc, const uint8_t* vc, const float* msc, const float* vsc, int64_t beg, int left,
+                                         int lane) {
         m_scale = msc[beg / kStateBlock];
         v_scale = vsc[beg / kStateBlock];
         if constexpr (kVectors) {
             const int64_t i = beg + lane * 8;
-            load8(a.g + i, g);
-            a.load8p(i, p);
+            g.load(a.g + i);
+            p.load(a.read() + i);
             const uint2 x = *reinterpret_cast<const uint2*>(mc + i), y = *reinterpret_cast<const uint2*>(vc + i);
             m[0] = x.x; m[1] = x.y; v[0] = y.x; v[1] = y.y;
         } else {
             m[0] = m[1] = v[0] = v[1] = 0;
+            float gg[8], pp[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int64_t i = beg + place(lane, e);
                 const bool there = place(lane, e) < left;
-                g[e] = there ? load1(a.g + i) : 0.f;
-                p[e] = there ? a.load1p(i) : 0.f;
+                gg[e] = there ? load1(a.g + i) : 0.f;
+                pp[e] = there ? load1(a.read() + i) : 0.f;
                 m[e / 4] |= (there ? static_cast<uint32_t>(mc[i]) : 0u) << (8 * (e % 4));
                 v[e / 4] |= (there ? static_cast<uint32_t>(vc[i]) : 0u) << (8 * (e % 4));
             }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { g1[e] = f2(gg[2 * e], gg[2 * e + 1]); p1[e] = f2(pp[2 * e], pp[2 * e + 1]); }
         }
     }
-    __device__ __forceinline__ void step(const AdamHyper& h, const Arrays<kParam, G>& a, uint8_t* mc, uint8_t* vc, float* msc, float* vsc, int64_t beg,
-                                         int left, int lane, uint32_t key) {
-        float fm[8], fv[8];
-        decode4<__NV_E4M3>(m[0], m_scale, fm);
-        decode4<__NV_E4M3>(m[1], m_scale, fm + 4);
-        decode4<__NV_E5M2>(v[0], v_scale, fv);
-        decode4<__NV_E5M2>(v[1], v_scale, fv + 4);
-        uint32_t most_m = 0, most_v = 0;
+    __device__ __forceinline__ void step(const AdamPairs& h, const A& a, uint8_t* mc, uint8_t* vc, float* msc, float* vsc, int64_t beg, int left, int lane,
+                                         uint32_t key) {
+        F2 fg[4], fp[4], fm[4], fv[4];
+        if constexpr (kVectors) {
+            g.get(fg);
+            p.get(fp);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            moments(h, g[e], fm[e], fv[e]);
-            p[e] = stepped(h, p[e], fm[e], fv[e]);
-            if (!kVectors && place(lane, e) >= left) fm[e] = fv[e] = 0.f;
-            most_m = max(most_m, __float_as_uint(fm[e]) & 0x7fffffffu);
-            most_v = max(most_v, __float_as_uint(fv[e]) & 0x7fffffffu);
+            for (int e = 0; e < 4; ++e) { fg[e] = g1[e]; fp[e] = p1[e]; }
         }
-        most_m = __reduce_max_sync(0xffffffffu, most_m);
-        most_v = __reduce_max_sync(0xffffffffu, most_v);
+        decode4<__NV_E4M3>(m[0], fm);
+        decode4<__NV_E4M3>(m[1], fm + 2);
+        decode4<__NV_E5M2>(v[0], fv);
+        decode4<__NV_E5M2>(v[1], fv + 2);
+        // (scale and beta in one factor: the scale is a power of two)
+        const F2 b1m = mul2(h.b1, both(m_scale)), b2v = mul2(h.b2, both(v_scale));
+        float top_m = 0.f, top_v = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            moments(h, fg[e], b1m, b2v, fm[e], fv[e]);
+            fp[e] = stepped(h, fp[e], fm[e], fv[e]);
+            if constexpr (!kVectors) {
+                const float2 x = split(fm[e]), y = split(fv[e]);
+                const bool one = place(lane, 2 * e) < left, two = place(lane, 2 * e + 1) < left;
+                fm[e] = f2(one ? x.x : 0.f, two ? x.y : 0.f);
+                fv[e] = f2(one ? y.x : 0.f, two ? y.y : 0.f);
+            }
+            const float2 x = split(fm[e]), y = split(fv[e]);
+            top_m = larger(larger(top_m, x.x), x.y);
+            top_v = larger(larger(top_v, y.x), y.y);
+        }
         constexpr uint32_t kInf = 0x7f800000u;
-        const bool finite = most_m < kInf && most_v < kInf;
-        if (!finite) {      // the largest of the finite ones
+        uint32_t most_m = __reduce_max_sync(0xffffffffu, __float_as_uint(top_m)), most_v = __reduce_max_sync(0xffffffffu, __float_as_uint(top_v));
+        uint32_t nan_m[2] = {0, 0}, nan_v[2] = {0, 0};
+        if (most_m >= kInf || most_v >= kInf) {      // what is not finite is taken as zero, and its codes as NaN in the end
             most_m = most_v = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const uint32_t x = __float_as_uint(fm[e]) & 0x7fffffffu, y = __float_as_uint(fv[e]) & 0x7fffffffu;
-                if (x < kInf) most_m = max(most_m, x);
-                if (y < kInf) most_v = max(most_v, y);
+                float2 x = split(fm[e / 2]), y = split(fv[e / 2]);
+                float& xe = e % 2 ? x.y : x.x;
+                float& ye = e % 2 ? y.y : y.x;
+                if ((__float_as_uint(xe) & 0x7fffffffu) >= kInf) { xe = 0.f; nan_m[e / 4] |= 0x7fu << (8 * (e % 4)); }
+                if ((__float_as_uint(ye) & 0x7fffffffu) >= kInf) { ye = 0.f; nan_v[e / 4] |= 0x7fu << (8 * (e % 4)); }
+                most_m = max(most_m, __float_as_uint(xe) & 0x7fffffffu);
+                most_v = max(most_v, __float_as_uint(ye));
+                fm[e / 2] = f2(x.x, x.y);
+                fv[e / 2] = f2(y.x, y.y);
             }
             most_m = __reduce_max_sync(0xffffffffu, most_m);
             most_v = __reduce_max_sync(0xffffffffu, most_v);
         }
         const int field_m = scale_field<E4M3>(most_m), field_v = scale_field<E5M2>(most_v);
-        m[0] = m[1] = v[0] = v[1] = 0;
+        const F2 over_m = both(__int_as_float((254 - field_m) << 23)), over_v = both(__int_as_float((254 - field_v) << 23));      // 1 / scale
+        const uint32_t least_v = static_cast<uint32_t>(field_v - 14) << 23;      // e5m2's smallest normal number, 2^-14
+        const F2 down = both(0x1p-120f), up = both(0x1p120f), zero = both(0.f);
+        const uint32_t beyond = key + static_cast<uint32_t>(beg >> 32) * kBeyond32;      // (a block lies on one side of 2^32)
+        const uint32_t first = ((static_cast<uint32_t>(beg) + static_cast<uint32_t>(lane) * 8) ^ (beyond & ~7u)) * kFirstRound;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int64_t i = beg + place(lane, e);
-            const uint32_t r = random_bits(key + static_cast<uint32_t>(i >> 32) * 0x9C2F1D35u, static_cast<uint32_t>(i));
-            const uint32_t x = __float_as_uint(fm[e]), size = x & 0x7fffffffu, y = __float_as_uint(fv[e]) & 0x7fffffffu;
-            uint32_t cm = coded<E4M3, false>(size, r & 0xffffu, field_m), cv = coded<E5M2, true>(y, r >> 16, field_v);
-            if (cm != 0) cm |= (x >> 24) & 0x80u;
-            if (!finite) {
-                if (size >= kInf) cm = 0x7fu;
-                if (y >= kInf) cv = 0x7fu;
+        for (int e = 0; e < 4; ++e) {
+            const float2 x = split(fm[e]), y = split(fv[e]);
+            uint32_t zm[2], zv[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int n = 2 * e + i;
+                // (eight places from a multiple of eight on differ from the key in three bits apart from the others, so the product is a sum)
+                const uint32_t start = kVectors ? first + ((beyond & 7u) ^ n) * kFirstRound
+                                                : ((static_cast<uint32_t>(beg) + static_cast<uint32_t>(place(lane, n))) ^ beyond) * kFirstRound;
+                const uint32_t r = random_bits(start), upper = r >> 16;
+                const uint32_t bits_m = __float_as_uint(i ? x.y : x.x), bits_v = __float_as_uint(i ? y.y : y.x);
+                zm[i] = rounded<E4M3>(bits_m, (r ^ upper) & 0xffffu);
+                zv[i] = max(rounded<E5M2>(bits_v, upper), min(bits_v, 1u) * least_v);
             }
-            m[e / 4] |= cm << (8 * (e % 4));
-            v[e / 4] |= cv << (8 * (e % 4));
+            // m below e4m3's smallest normal number, 2^-6, becomes zero: that is 2^-126 in between (and minus zero plus zero is zero)
+            const F2 sm = mul2(f2(__uint_as_float(zm[0]), __uint_as_float(zm[1])), over_m);
+            fm[e] = fma2(mul2_flush(sm, down), up, zero);
+            fv[e] = mul2(f2(__uint_as_float(zv[0]), __uint_as_float(zv[1])), over_v);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            m[i] = encode4<__NV_E4M3>(fm[2 * i], fm[2 * i + 1]) | nan_m[i];
+            v[i] = encode4<__NV_E5M2>(fv[2 * i], fv[2 * i + 1]) | nan_v[i];
         }
         if (lane == 0) {
             msc[beg / kStateBlock] = __int_as_float(field_m << 23);
@@ -330,7 +415,7 @@ struct StateBlock {
             const int64_t i = beg + lane * 8;
             *reinterpret_cast<uint2*>(mc + i) = make_uint2(m[0], m[1]);
             *reinterpret_cast<uint2*>(vc + i) = make_uint2(v[0], v[1]);
-            a.store8p(i, p);
+            a.store8p(i, fp);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -338,16 +423,18 @@ struct StateBlock {
                 if (place(lane, e) >= left) continue;
                 mc[i] = static_cast<uint8_t>(m[e / 4] >> (8 * (e % 4)));
                 vc[i] = static_cast<uint8_t>(v[e / 4] >> (8 * (e % 4)));
-                a.store1p(i, p[e]);
+                const float2 x = split(fp[e / 2]);
+                a.store1p(i, e % 2 ? x.y : x.x);
             }
         }
     }
 };
 
 template <int kMost, int kParam, typename G>
-__global__ void __launch_bounds__(kAdamThreads) adamw8_kernel(const __grid_constant__ AdamTable<kMost> tb, const AdamHyper hyper) {
+__global__ void __launch_bounds__(kAdamThreads, 3) adamw8_kernel(const __grid_constant__ AdamTable<kMost> tb, const AdamHyper hyper) {
     const int chunk = blockIdx.x, t = tensor_of(tb, chunk), local = chunk - tb.chunk_prefix[t];
     const AdamHyper h = resolved(hyper);
+    const AdamPairs hp(h);
     using P = typename ParamType<kParam>::T;
     const Arrays<kParam, G> a{static_cast<P*>(tb.p[t]), tb.master[t], static_cast<const G*>(tb.g[t])};
     uint8_t* const mc = static_cast<uint8_t*>(tb.m[t]);
@@ -363,7 +450,7 @@ __global__ void __launch_bounds__(kAdamThreads) adamw8_kernel(const __grid_const
         for (int u = 0; u < kAdamDeep; ++u) b[u].load(a, mc, vc, tb.m_scale[t], tb.v_scale[t], beg + u * kApart, kStateBlock, lane);
 #pragma unroll
         for (int u = 0; u < kAdamDeep; ++u)
-            b[u].step(h, a, mc, vc, tb.m_scale[t], tb.v_scale[t], beg + u * kApart, kStateBlock, lane, key);
+            b[u].step(hp, a, mc, vc, tb.m_scale[t], tb.v_scale[t], beg + u * kApart, kStateBlock, lane, key);
         return;
     }
 #pragma unroll 1
@@ -373,7 +460,7 @@ __global__ void __launch_bounds__(kAdamThreads) adamw8_kernel(const __grid_const
         const int left = n - at < kStateBlock ? static_cast<int>(n - at) : kStateBlock;
         StateBlock<kParam, G, false> b;
         b.load(a, mc, vc, tb.m_scale[t], tb.v_scale[t], at, left, lane);
-        b.step(h, a, mc, vc, tb.m_scale[t], tb.v_scale[t], at, left, lane, key);
+        b.step(hp, a, mc, vc, tb.m_scale[t], tb.v_scale[t], at, left, lane, key);
     }
 }
 
@@ -481,7 +568,7 @@ extern "C" int pf_adamw_step(void* const* params, float* const* masters, const v
     h.c1 = static_cast<float>(1.0 - o.beta1);
     h.b2 = static_cast<float>(o.beta2);
     h.c2 = static_cast<float>(1.0 - o.beta2);
-    h.eps = static_cast<float>(o.eps);
+    h.eps = std::fmax(static_cast<float>(o.eps), 0x1p-63f);
     h.wd = static_cast<float>(o.weight_decay);
     h.scalars = scalars;
     if (!scalars) {

@@ -12,6 +12,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "pf_f32x2.cuh"
 #include "pf_internal.h"
 
 namespace pf {
@@ -83,32 +84,6 @@ __device__ __forceinline__ float get1(const __nv_bfloat16* p) { return __bfloat1
 __device__ __forceinline__ void put1(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put1(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
-// Two fp32 numbers that one instruction works on.
-struct F2 {
-    uint64_t v;
-};
-__device__ __forceinline__ F2 f2(float x, float y) {
-    F2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ float2 split(F2 a) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
-    return r;
-}
-__device__ __forceinline__ F2 mul(F2 a, F2 b) {
-    F2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-    F2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
-__device__ __forceinline__ F2 negated(F2 a) { return F2{a.v ^ 0x8000000080000000ull}; }
-
 template <typename T> struct Piece;      // 16 bytes: kN elements, kN / 2 pairs of neighbours
 template <> struct Piece<float> {
     static constexpr int kN = 4;
@@ -162,8 +137,8 @@ __device__ __forceinline__ void turn(F2 (&a)[kN / 2], F2 (&b)[kN / 2], const F2 
 #pragma unroll
         for (int i = 0; i < kN / 2; ++i) {
             const F2 x = a[i], y = b[i];
-            a[i] = fma2(kBack ? y : negated(y), s[i], mul(x, c[i]));
-            b[i] = fma2(kBack ? negated(x) : x, s[i], mul(y, c[i]));
+            a[i] = fma2(kBack ? y : negated(y), s[i], mul2(x, c[i]));
+            b[i] = fma2(kBack ? negated(x) : x, s[i], mul2(y, c[i]));
         }
     }
 }
@@ -329,7 +304,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
             }
             xa.get(a);
             xb.get(b);
-            F2 sq2 = mul(a[0], a[0]);
+            F2 sq2 = mul2(a[0], a[0]);
 #pragma unroll
             for (int i = 1; i < kN / 2; ++i) sq2 = fma2(a[i], a[i], sq2);
 #pragma unroll
@@ -341,7 +316,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
             const F2 rr = f2(r, r);
             if constexpr (!kBwd) {
 #pragma unroll
-                for (int i = 0; i < kN / 2; ++i) { a[i] = mul(a[i], mul(rr, wa[i])); b[i] = mul(b[i], mul(rr, wb[i])); }
+                for (int i = 0; i < kN / 2; ++i) { a[i] = mul2(a[i], mul2(rr, wa[i])); b[i] = mul2(b[i], mul2(rr, wb[i])); }
                 turn<kN, kPairs, false>(a, b, c, sn);
             } else {
                 F2 ea[kN / 2], eb[kN / 2];
@@ -357,19 +332,19 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
                 F2 dot2 = f2(0.f, 0.f);
 #pragma unroll
                 for (int i = 0; i < kN / 2; ++i) {
-                    a[i] = mul(a[i], rr);
-                    b[i] = mul(b[i], rr);
+                    a[i] = mul2(a[i], rr);
+                    b[i] = mul2(b[i], rr);
                     dwa[i] = fma2(ea[i], a[i], dwa[i]);
                     dwb[i] = fma2(eb[i], b[i], dwb[i]);
-                    ea[i] = mul(ea[i], wa[i]);
-                    eb[i] = mul(eb[i], wb[i]);
+                    ea[i] = mul2(ea[i], wa[i]);
+                    eb[i] = mul2(eb[i], wb[i]);
                     dot2 = fma2(ea[i], a[i], fma2(eb[i], b[i], dot2));
                 }
                 const float2 d = split(dot2);
                 const float dot = -sum_lanes<kLanes>(d.x + d.y) * inv_dim;
                 const F2 dd = f2(dot, dot);
 #pragma unroll
-                for (int i = 0; i < kN / 2; ++i) { a[i] = mul(rr, fma2(a[i], dd, ea[i])); b[i] = mul(rr, fma2(b[i], dd, eb[i])); }
+                for (int i = 0; i < kN / 2; ++i) { a[i] = mul2(rr, fma2(a[i], dd, ea[i])); b[i] = mul2(rr, fma2(b[i], dd, eb[i])); }
             }
             if (on) {
                 Piece<T>::store(out + ia, a);
