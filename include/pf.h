@@ -428,7 +428,8 @@ int pf_qk_norm_rope_bwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
  * numels[i] elements, t = step:
  *   g = grad_scale * grad        m <- beta1 m + (1 - beta1) g        v <- beta2 v + (1 - beta2) g^2
  *   p <- p - lr (weight_decay p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
- * in fp32, m and v with each product and sum rounded by itself; an eps below 2^-63 counts as 2^-63.
+ * in fp32, m and v with each product and sum rounded by itself; eps sqrt(1 - beta2^t) below 2^-63
+ * counts as 2^-63.
  *   params   in param_dtype.  masters: NULL, or (PF_BF16 parameters) fp32 masters, which are then what is read and stepped;
  *            params receives them rounded.  Without masters a PF_BF16 parameter is stepped in fp32 and rounded once.
  *   grads    in grad_dtype, read only: the slices of a flat buffer as they are (element alignment) or any other tensors

@@ -27,12 +27,14 @@
 namespace pf {
 namespace {
 
-constexpr int kAdamThreads = 256, kAdamWarps = kAdamThreads / 32;
+constexpr int kAdamThreads = 256;
 constexpr int kAdamVec = 8;                    // elements of a thread at a time
 constexpr int kAdamDeep = 2;                   // such pieces in flight
-constexpr int kAdamChunk = kAdamThreads * kAdamVec * kAdamDeep;
+constexpr int kAdamPiece = kAdamThreads * kAdamVec;      // elements of a block at a time; it takes AdamTable::steps of them
 constexpr int kStateBlock = 256;               // elements that share a scale: one piece of a warp
 constexpr int kNoVectors = -1;                 // AdamTable::head of a tensor whose arrays never come to 16-byte boundaries together
+
+constexpr int kAdamStarts = 64;
 
 enum ParamKind : int { P_F32 = 0, P_BF16 = 1, P_MASTER = 2 };      // P_MASTER: bf16 parameters that follow fp32 masters
 
@@ -50,16 +52,31 @@ struct AdamTable {
     int chunk_prefix[kMost + 1];
     signed char head[kMost];      // elements in front of the first one at which every array is at a 16-byte boundary
     int first, count;             // place of tensor 0 in the caller's list
+    int steps;
+    unsigned char start[kAdamStarts];      // the tensor of chunk i << start_shift
+    int start_shift;
 };
 
+// p <- p - lr (wd p + (m r1) / (sqrt(v r2) + eps)), r = 1 / (1 - beta^t), is p - pace (decay p + m / (sqrt(v) + eps / sqrt(r2))) with
+// pace = lr r1 / sqrt(r2).
 struct AdamHyper {
     float b1, c1, b2, c2, eps, wd;
-    float lr, r1, r2, grad_scale;      // r1 = 1 / (1 - beta1^t), r2 likewise
+    float pace, decay, floor, grad_scale;      // floor = eps / sqrt(r2), at least 2^-63
     uint32_t seed;
-    const pf_adamw_scalars* scalars;   // replace lr, r1, r2, grad_scale and seed
+    const pf_adamw_scalars* scalars;           // replace the last row and the seed
+    template <typename R>
+    __host__ __device__ void settle(R lr, R correction1, R correction2, float scale, uint32_t bits) {
+        const R root = sqrt(correction2), speed = root / correction1;
+        pace = static_cast<float>(lr * speed);
+        decay = pace != 0.f ? static_cast<float>(wd / speed) : 0.f;
+        floor = static_cast<float>(eps * root);
+        floor = floor > 0x1p-63f ? floor : 0x1p-63f;
+        grad_scale = scale;
+        seed = bits;
+    }
 };
 
-// (Operands below the normal numbers count as zero: eps is at least 2^-63, the root of the smallest normal number.)
+// (Operands below the normal numbers count as zero: the floor is at least 2^-63, the root of the smallest normal number.)
 __device__ __forceinline__ float sqrt_fast(float x) {
     float y;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -74,10 +91,10 @@ __device__ __forceinline__ F2 both(float x) { return f2(x, x); }
 
 // The hyperparameters as pairs of fp32 numbers.
 struct AdamPairs {
-    F2 b1, c1, b2, c2, eps, wd, minus_lr, r1, r2, grad_scale;
+    F2 b1, c1, b2, c2, floor, decay, minus_pace, grad_scale;
     __device__ __forceinline__ explicit AdamPairs(const AdamHyper& h)
-        : b1(both(h.b1)), c1(both(h.c1)), b2(both(h.b2)), c2(both(h.c2)), eps(both(h.eps)), wd(both(h.wd)), minus_lr(both(-h.lr)), r1(both(h.r1)),
-          r2(both(h.r2)), grad_scale(both(h.grad_scale)) {}
+        : b1(both(h.b1)), c1(both(h.c1)), b2(both(h.b2)), c2(both(h.c2)), floor(both(h.floor)), decay(both(h.decay)), minus_pace(both(-h.pace)),
+          grad_scale(both(h.grad_scale)) {}
 };
 // m and v of two elements after the step; b1m = beta1 times a power of two where m is in units of that (and b2v).
 __device__ __forceinline__ void moments(const AdamPairs& h, F2 grad, F2 b1m, F2 b2v, F2& m, F2& v) {
@@ -87,10 +104,9 @@ __device__ __forceinline__ void moments(const AdamPairs& h, F2 grad, F2 b1m, F2 
     v = add2(fma2(v, b2v, zero), fma2(mul2(g, g), h.c2, zero));
 }
 __device__ __forceinline__ F2 stepped(const AdamPairs& h, F2 p, F2 m, F2 v) {
-    const float2 w = split(mul2(v, h.r2));
-    const float2 d = split(add2(f2(sqrt_fast(w.x), sqrt_fast(w.y)), h.eps));
-    const F2 u = mul2(mul2(m, h.r1), f2(rcp_fast(d.x), rcp_fast(d.y)));
-    return fma2(h.minus_lr, fma2(h.wd, p, u), p);
+    const float2 w = split(v);
+    const float2 d = split(add2(f2(sqrt_fast(w.x), sqrt_fast(w.y)), h.floor));
+    return fma2(h.minus_pace, fma2(h.decay, p, mul2(m, f2(rcp_fast(d.x), rcp_fast(d.y)))), p);
 }
 
 __device__ __forceinline__ float bf16_to_f32(unsigned short raw) { return __uint_as_float(static_cast<unsigned>(raw) << 16); }
@@ -160,23 +176,17 @@ struct Arrays {
 
 template <int kMost>
 __device__ __forceinline__ int tensor_of(const AdamTable<kMost>& tb, int chunk) {
-    int lo = 0, hi = tb.count;      // chunk_prefix[lo] <= chunk < chunk_prefix[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (tb.chunk_prefix[mid] <= chunk) lo = mid; else hi = mid;
-    }
-    return lo;
+    int t = tb.start[chunk >> tb.start_shift];
+    while (tb.chunk_prefix[t + 1] <= chunk) ++t;
+    return t;
 }
 // The hyperparameters of this launch, once the kernel before has completed.
 __device__ __forceinline__ AdamHyper resolved(AdamHyper h) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (h.scalars) {
-        h.lr = h.scalars->lr;
-        h.r1 = 1.f / h.scalars->correction1;
-        h.r2 = 1.f / h.scalars->correction2;
-        h.grad_scale = h.scalars->grad_scale;
-        h.seed = h.scalars->seed;
+        const pf_adamw_scalars& o = *h.scalars;
+        h.settle<float>(o.lr, o.correction1, o.correction2, o.grad_scale, o.seed);
     }
     return h;
 }
@@ -203,7 +213,7 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     };
     const int head = tb.head[t];
     if (head == kNoVectors) {
-        const int64_t beg = static_cast<int64_t>(local) * kAdamChunk, end = beg + kAdamChunk < n ? beg + kAdamChunk : n;
+        const int64_t beg = static_cast<int64_t>(local) * tb.steps * kAdamPiece, end = min(n, beg + tb.steps * kAdamPiece);
 #pragma unroll 4
         for (int64_t i = beg + threadIdx.x; i < end; i += kAdamThreads) single(i);
         return;
@@ -214,32 +224,34 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
         const int64_t i = head + vectors * kAdamVec + threadIdx.x;
         if (i < n) single(i);
     }
-    const int64_t first = static_cast<int64_t>(local) * (kAdamThreads * kAdamDeep) + threadIdx.x;
-    Eight<G> g[kAdamDeep];
-    Eight<float> m[kAdamDeep], v[kAdamDeep];
-    Eight<typename Arrays<kParam, G>::R> p[kAdamDeep];
+    const int64_t mine = static_cast<int64_t>(local) * tb.steps * kAdamThreads, last = min(vectors, mine + tb.steps * kAdamThreads);
+    for (int64_t k = mine + threadIdx.x; k < last; k += kAdamDeep * kAdamThreads) {
+        Eight<G> g[kAdamDeep];
+        Eight<float> m[kAdamDeep], v[kAdamDeep];
+        Eight<typename Arrays<kParam, G>::R> p[kAdamDeep];
 #pragma unroll
-    for (int u = 0; u < kAdamDeep; ++u) {
-        const int64_t k = first + u * kAdamThreads, i = head + k * kAdamVec;
-        if (k < vectors) { g[u].load(a.g + i); m[u].load(ms + i); v[u].load(vs + i); p[u].load(a.read() + i); }
-    }
-#pragma unroll
-    for (int u = 0; u < kAdamDeep; ++u) {
-        const int64_t k = first + u * kAdamThreads, i = head + k * kAdamVec;
-        if (k >= vectors) break;
-        F2 fg[4], fm[4], fv[4], fp[4];
-        g[u].get(fg);
-        m[u].get(fm);
-        v[u].get(fv);
-        p[u].get(fp);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            moments(hp, fg[e], hp.b1, hp.b2, fm[e], fv[e]);
-            fp[e] = stepped(hp, fp[e], fm[e], fv[e]);
+        for (int u = 0; u < kAdamDeep; ++u) {
+            const int64_t i = head + (k + u * kAdamThreads) * kAdamVec;
+            if (k + u * kAdamThreads < last) { g[u].load(a.g + i); m[u].load(ms + i); v[u].load(vs + i); p[u].load(a.read() + i); }
         }
-        Eight<float>::store(ms + i, fm);
-        Eight<float>::store(vs + i, fv);
-        a.store8p(i, fp);
+#pragma unroll
+        for (int u = 0; u < kAdamDeep; ++u) {
+            const int64_t i = head + (k + u * kAdamThreads) * kAdamVec;
+            if (k + u * kAdamThreads >= last) break;
+            F2 fg[4], fm[4], fv[4], fp[4];
+            g[u].get(fg);
+            m[u].get(fm);
+            v[u].get(fv);
+            p[u].get(fp);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                moments(hp, fg[e], hp.b1, hp.b2, fm[e], fv[e]);
+                fp[e] = stepped(hp, fp[e], fm[e], fv[e]);
+            }
+            Eight<float>::store(ms + i, fm);
+            Eight<float>::store(vs + i, fv);
+            a.store8p(i, fp);
+        }
     }
 }
 
@@ -342,6 +354,7 @@ struct StateBlock {
         // (scale and beta in one factor: the scale is a power of two)
         const F2 b1m = mul2(h.b1, both(m_scale)), b2v = mul2(h.b2, both(v_scale));
         float top_m = 0.f, top_v = 0.f;
+        uint32_t low_v = 0xffffffffu;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             moments(h, fg[e], b1m, b2v, fm[e], fv[e]);
@@ -355,6 +368,7 @@ struct StateBlock {
             const float2 x = split(fm[e]), y = split(fv[e]);
             top_m = larger(larger(top_m, x.x), x.y);
             top_v = larger(larger(top_v, y.x), y.y);
+            low_v = min(min(low_v, __float_as_uint(y.x)), __float_as_uint(y.y));
         }
         constexpr uint32_t kInf = 0x7f800000u;
         uint32_t most_m = __reduce_max_sync(0xffffffffu, __float_as_uint(top_m)), most_v = __reduce_max_sync(0xffffffffu, __float_as_uint(top_v));
@@ -379,6 +393,8 @@ struct StateBlock {
         const int field_m = scale_field<E4M3>(most_m), field_v = scale_field<E5M2>(most_v);
         const F2 over_m = both(__int_as_float((254 - field_m) << 23)), over_v = both(__int_as_float((254 - field_v) << 23));      // 1 / scale
         const uint32_t least_v = static_cast<uint32_t>(field_v - 14) << 23;      // e5m2's smallest normal number, 2^-14
+        // (few blocks have a v that small, or none: without one the rounded values need no limit)
+        const bool small_v = __any_sync(0xffffffffu, low_v < least_v);
         const F2 down = both(0x1p-120f), up = both(0x1p120f), zero = both(0.f);
         const uint32_t beyond = key + static_cast<uint32_t>(beg >> 32) * kBeyond32;      // (a block lies on one side of 2^32)
         const uint32_t first = ((static_cast<uint32_t>(beg) + static_cast<uint32_t>(lane) * 8) ^ (beyond & ~7u)) * kFirstRound;
@@ -395,7 +411,8 @@ struct StateBlock {
                 const uint32_t r = random_bits(start), upper = r >> 16;
                 const uint32_t bits_m = __float_as_uint(i ? x.y : x.x), bits_v = __float_as_uint(i ? y.y : y.x);
                 zm[i] = rounded<E4M3>(bits_m, (r ^ upper) & 0xffffu);
-                zv[i] = max(rounded<E5M2>(bits_v, upper), min(bits_v, 1u) * least_v);
+                zv[i] = rounded<E5M2>(bits_v, upper);
+                if (small_v) zv[i] = max(zv[i], min(bits_v, 1u) * least_v);
             }
             // m below e4m3's smallest normal number, 2^-6, becomes zero: that is 2^-126 in between (and minus zero plus zero is zero)
             const F2 sm = mul2(f2(__uint_as_float(zm[0]), __uint_as_float(zm[1])), over_m);
@@ -431,7 +448,7 @@ struct StateBlock {
 };
 
 template <int kMost, int kParam, typename G>
-__global__ void __launch_bounds__(kAdamThreads, 3) adamw8_kernel(const __grid_constant__ AdamTable<kMost> tb, const AdamHyper hyper) {
+__global__ void __launch_bounds__(kAdamThreads, 4) adamw8_kernel(const __grid_constant__ AdamTable<kMost> tb, const AdamHyper hyper) {
     const int chunk = blockIdx.x, t = tensor_of(tb, chunk), local = chunk - tb.chunk_prefix[t];
     const AdamHyper h = resolved(hyper);
     const AdamPairs hp(h);
@@ -442,25 +459,32 @@ __global__ void __launch_bounds__(kAdamThreads, 3) adamw8_kernel(const __grid_co
     const int64_t n = tb.n[t];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const uint32_t key = tensor_key(h.seed, tb.first + t);
-    const int64_t beg = static_cast<int64_t>(local) * kAdamChunk + warp * kStateBlock;
-    constexpr int kApart = kAdamWarps * kStateBlock;
-    if (tb.head[t] == 0 && beg + (kAdamDeep - 1) * kApart + kStateBlock <= n) {
-        StateBlock<kParam, G, true> b[kAdamDeep];
+    float* const msc = tb.m_scale[t];
+    float* const vsc = tb.v_scale[t];
+    const int64_t beg = static_cast<int64_t>(local) * tb.steps * kAdamPiece + warp * kStateBlock;
+    const int64_t last = min(n, beg - warp * kStateBlock + tb.steps * kAdamPiece);
+    int64_t at = beg;
+    if (tb.head[t] == 0) {      // whole blocks, two at a time
+#pragma unroll 1
+        for (; at + (kAdamDeep - 1) * kAdamPiece + kStateBlock <= last; at += kAdamDeep * kAdamPiece) {
+            StateBlock<kParam, G, true> b[kAdamDeep];
 #pragma unroll
-        for (int u = 0; u < kAdamDeep; ++u) b[u].load(a, mc, vc, tb.m_scale[t], tb.v_scale[t], beg + u * kApart, kStateBlock, lane);
+            for (int u = 0; u < kAdamDeep; ++u) b[u].load(a, mc, vc, msc, vsc, at + u * kAdamPiece, kStateBlock, lane);
 #pragma unroll
-        for (int u = 0; u < kAdamDeep; ++u)
-            b[u].step(hp, a, mc, vc, tb.m_scale[t], tb.v_scale[t], beg + u * kApart, kStateBlock, lane, key);
-        return;
+            for (int u = 0; u < kAdamDeep; ++u) b[u].step(hp, a, mc, vc, msc, vsc, at + u * kAdamPiece, kStateBlock, lane, key);
+        }
+        for (; at + kStateBlock <= last; at += kAdamPiece) {
+            StateBlock<kParam, G, true> b;
+            b.load(a, mc, vc, msc, vsc, at, kStateBlock, lane);
+            b.step(hp, a, mc, vc, msc, vsc, at, kStateBlock, lane, key);
+        }
     }
 #pragma unroll 1
-    for (int u = 0; u < kAdamDeep; ++u) {
-        const int64_t at = beg + u * kApart;
-        if (at >= n) break;
+    for (; at < last; at += kAdamPiece) {
         const int left = n - at < kStateBlock ? static_cast<int>(n - at) : kStateBlock;
         StateBlock<kParam, G, false> b;
-        b.load(a, mc, vc, tb.m_scale[t], tb.v_scale[t], at, left, lane);
-        b.step(hp, a, mc, vc, tb.m_scale[t], tb.v_scale[t], at, left, lane, key);
+        b.load(a, mc, vc, msc, vsc, at, left, lane);
+        b.step(hp, a, mc, vc, msc, vsc, at, left, lane, key);
     }
 }
 
@@ -493,16 +517,23 @@ int head_of(const AdamList& l, int i) {
     return kNoVectors;
 }
 
+constexpr int kAdamFill = 8;      // blocks of an SM, those that wait for their turn among them
 template <int kMost, int kParam, typename G>
 cudaError_t adamw_by(const AdamList& l, const AdamHyper& h, cudaStream_t stream) {
+    int64_t pieces = 0;
+    for (int i = 0; i < l.count; ++i) pieces += ceil_div(l.n[i], kAdamPiece);
+    // a block takes several pieces where enough blocks are left for every SM
+    const int64_t fill = static_cast<int64_t>(num_sms()) * kAdamFill;
+    const int steps = pieces >= 2 * fill ? 2 : 1;
     int i = 0;
     while (i < l.count) {
         AdamTable<kMost> tb;
         tb.count = 0;
         tb.first = i;
         tb.chunk_prefix[0] = 0;
+        tb.steps = steps;
         for (; i < l.count && i - tb.first < kMost; ++i) {      // (empty tensors keep their place)
-            const int64_t chunks = ceil_div(l.n[i], kAdamChunk);
+            const int64_t chunks = ceil_div(l.n[i], static_cast<int64_t>(steps) * kAdamPiece);
             if (tb.chunk_prefix[tb.count] + chunks > 0x7fffffff) break;
             const int c = tb.count++;
             tb.p[c] = l.p[i];
@@ -519,6 +550,13 @@ cudaError_t adamw_by(const AdamList& l, const AdamHyper& h, cudaStream_t stream)
         if (tb.count == 0) return cudaErrorInvalidValue;
         const int blocks = tb.chunk_prefix[tb.count];
         if (blocks == 0) continue;
+        tb.start_shift = 0;
+        while ((blocks - 1) >> tb.start_shift >= kAdamStarts) ++tb.start_shift;
+        for (int c = 0, t = 0; c < blocks; c += 1 << tb.start_shift) {
+            while (tb.chunk_prefix[t + 1] <= c) ++t;
+            tb.start[c >> tb.start_shift] = static_cast<unsigned char>(t);
+            if (c > 0x7fffffff - (1 << tb.start_shift)) break;
+        }
         const auto kernel = l.state8 ? adamw8_kernel<kMost, kParam, G> : adamw_kernel<kMost, kParam, G>;
         const cudaError_t e = launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kAdamThreads, 0, 1, stream, tb, h);
         if (e != cudaSuccess) return e;
@@ -568,15 +606,12 @@ extern "C" int pf_adamw_step(void* const* params, float* const* masters, const v
     h.c1 = static_cast<float>(1.0 - o.beta1);
     h.b2 = static_cast<float>(o.beta2);
     h.c2 = static_cast<float>(1.0 - o.beta2);
-    h.eps = std::fmax(static_cast<float>(o.eps), 0x1p-63f);
+    h.eps = static_cast<float>(o.eps);
     h.wd = static_cast<float>(o.weight_decay);
     h.scalars = scalars;
     if (!scalars) {
-        h.lr = static_cast<float>(o.lr);
-        h.r1 = static_cast<float>(1.0 / (1.0 - std::pow(o.beta1, static_cast<double>(o.step))));
-        h.r2 = static_cast<float>(1.0 / (1.0 - std::pow(o.beta2, static_cast<double>(o.step))));
-        h.grad_scale = o.grad_scale;
-        h.seed = o.seed;
+        const double t = static_cast<double>(o.step);
+        h.settle<double>(o.lr, 1.0 - std::pow(o.beta1, t), 1.0 - std::pow(o.beta2, t), o.grad_scale, o.seed);
     }
     const AdamList l{params, masters, grads, m, v, m_scales, v_scales, numels, count, param_dtype, grad_dtype, state8};
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
