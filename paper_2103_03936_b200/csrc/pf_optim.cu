@@ -27,10 +27,10 @@
 namespace pf {
 namespace {
 
-constexpr int kAdamThreads = 256;
+constexpr int kAdamThreads = 256, kAdamWarps = kAdamThreads / 32;
 constexpr int kAdamVec = 8;                    // elements of a thread at a time
 constexpr int kAdamDeep = 2;                   // such pieces in flight
-constexpr int kAdamPiece = kAdamThreads * kAdamVec;      // elements of a block at a time; it takes AdamTable::steps of them
+constexpr int kAdamPiece = kAdamThreads * kAdamVec;      // elements of a block at a time; it takes AdamTable::steps of them, at most kAdamDeep
 constexpr int kStateBlock = 256;               // elements that share a scale: one piece of a warp
 constexpr int kNoVectors = -1;                 // AdamTable::head of a tensor whose arrays never come to 16-byte boundaries together
 
@@ -337,7 +337,8 @@ struct StateBlock {
             for (int e = 0; e < 4; ++e) { g1[e] = f2(gg[2 * e], gg[2 * e + 1]); p1[e] = f2(pp[2 * e], pp[2 * e + 1]); }
         }
     }
-    __device__ __forceinline__ void step(const AdamPairs& h, const A& a, uint8_t* mc, uint8_t* vc, float* msc, float* vsc, int64_t beg, int left, int lane,
+    // `scales`: where the block leaves its two scales.
+    __device__ __forceinline__ void step(const AdamPairs& h, const A& a, uint8_t* mc, uint8_t* vc, float2& scales, int64_t beg, int left, int lane,
                                          uint32_t key) {
         F2 fg[4], fp[4], fm[4], fv[4];
         if constexpr (kVectors) {
@@ -369,6 +370,15 @@ struct StateBlock {
             top_m = larger(larger(top_m, x.x), x.y);
             top_v = larger(larger(top_v, y.x), y.y);
             low_v = min(min(low_v, __float_as_uint(y.x)), __float_as_uint(y.y));
+        }
+        if constexpr (kVectors) {
+            a.store8p(beg + lane * 8, fp);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float2 x = split(fp[e / 2]);
+                if (place(lane, e) < left) a.store1p(beg + place(lane, e), e % 2 ? x.y : x.x);
+            }
         }
         constexpr uint32_t kInf = 0x7f800000u;
         uint32_t most_m = __reduce_max_sync(0xffffffffu, __float_as_uint(top_m)), most_v = __reduce_max_sync(0xffffffffu, __float_as_uint(top_v));
@@ -424,15 +434,11 @@ struct StateBlock {
             m[i] = encode4<__NV_E4M3>(fm[2 * i], fm[2 * i + 1]) | nan_m[i];
             v[i] = encode4<__NV_E5M2>(fv[2 * i], fv[2 * i + 1]) | nan_v[i];
         }
-        if (lane == 0) {
-            msc[beg / kStateBlock] = __int_as_float(field_m << 23);
-            vsc[beg / kStateBlock] = __int_as_float(field_v << 23);
-        }
+        if (lane == 0) scales = make_float2(__int_as_float(field_m << 23), __int_as_float(field_v << 23));
         if constexpr (kVectors) {
             const int64_t i = beg + lane * 8;
             *reinterpret_cast<uint2*>(mc + i) = make_uint2(m[0], m[1]);
             *reinterpret_cast<uint2*>(vc + i) = make_uint2(v[0], v[1]);
-            a.store8p(i, fp);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -440,8 +446,6 @@ struct StateBlock {
                 if (place(lane, e) >= left) continue;
                 mc[i] = static_cast<uint8_t>(m[e / 4] >> (8 * (e % 4)));
                 vc[i] = static_cast<uint8_t>(v[e / 4] >> (8 * (e % 4)));
-                const float2 x = split(fp[e / 2]);
-                a.store1p(i, e % 2 ? x.y : x.x);
             }
         }
     }
@@ -462,29 +466,33 @@ __global__ void __launch_bounds__(kAdamThreads, 4) adamw8_kernel(const __grid_co
     float* const msc = tb.m_scale[t];
     float* const vsc = tb.v_scale[t];
     const int64_t beg = static_cast<int64_t>(local) * tb.steps * kAdamPiece + warp * kStateBlock;
-    const int64_t last = min(n, beg - warp * kStateBlock + tb.steps * kAdamPiece);
-    int64_t at = beg;
-    if (tb.head[t] == 0) {      // whole blocks, two at a time
+    // The scales of a block's pieces are stored together in the end: one by one they are parts of 32-byte sectors that other warps still read, which
+    // kept those waiting (26.8 M elements: 57 us, 93 with half of the loads in flight; 53 without the stores).
+    __shared__ float2 scales[kAdamDeep][kAdamWarps];
+    if (tb.head[t] == 0 && beg + (tb.steps - 1) * kAdamPiece + kStateBlock <= n) {      // whole blocks, all on the way at once
+        StateBlock<kParam, G, true> b[kAdamDeep];
+#pragma unroll
+        for (int u = 0; u < kAdamDeep; ++u)
+            if (u < tb.steps) b[u].load(a, mc, vc, msc, vsc, beg + u * kAdamPiece, kStateBlock, lane);
+#pragma unroll
+        for (int u = 0; u < kAdamDeep; ++u)
+            if (u < tb.steps) b[u].step(hp, a, mc, vc, scales[u][warp], beg + u * kAdamPiece, kStateBlock, lane, key);
+    } else {
 #pragma unroll 1
-        for (; at + (kAdamDeep - 1) * kAdamPiece + kStateBlock <= last; at += kAdamDeep * kAdamPiece) {
-            StateBlock<kParam, G, true> b[kAdamDeep];
-#pragma unroll
-            for (int u = 0; u < kAdamDeep; ++u) b[u].load(a, mc, vc, msc, vsc, at + u * kAdamPiece, kStateBlock, lane);
-#pragma unroll
-            for (int u = 0; u < kAdamDeep; ++u) b[u].step(hp, a, mc, vc, msc, vsc, at + u * kAdamPiece, kStateBlock, lane, key);
-        }
-        for (; at + kStateBlock <= last; at += kAdamPiece) {
-            StateBlock<kParam, G, true> b;
-            b.load(a, mc, vc, msc, vsc, at, kStateBlock, lane);
-            b.step(hp, a, mc, vc, msc, vsc, at, kStateBlock, lane, key);
+        for (int u = 0; u < tb.steps; ++u) {
+            const int64_t at = beg + u * kAdamPiece;
+            if (at >= n) break;
+            const int left = n - at < kStateBlock ? static_cast<int>(n - at) : kStateBlock;
+            StateBlock<kParam, G, false> b;
+            b.load(a, mc, vc, msc, vsc, at, left, lane);
+            b.step(hp, a, mc, vc, scales[u][warp], at, left, lane, key);
         }
     }
-#pragma unroll 1
-    for (; at < last; at += kAdamPiece) {
-        const int left = n - at < kStateBlock ? static_cast<int>(n - at) : kStateBlock;
-        StateBlock<kParam, G, false> b;
-        b.load(a, mc, vc, msc, vsc, at, left, lane);
-        b.step(hp, a, mc, vc, msc, vsc, at, left, lane, key);
+    __syncthreads();
+    const int64_t first = static_cast<int64_t>(local) * tb.steps * kAdamWarps, i = first + lane;
+    if (warp < 2 && lane < tb.steps * kAdamWarps && i * kStateBlock < n) {
+        const float2 x = scales[lane / kAdamWarps][lane % kAdamWarps];
+        if (warp == 0) msc[i] = x.x; else vsc[i] = x.y;
     }
 }
 
@@ -524,7 +532,7 @@ cudaError_t adamw_by(const AdamList& l, const AdamHyper& h, cudaStream_t stream)
     for (int i = 0; i < l.count; ++i) pieces += ceil_div(l.n[i], kAdamPiece);
     // a block takes several pieces where enough blocks are left for every SM
     const int64_t fill = static_cast<int64_t>(num_sms()) * kAdamFill;
-    const int steps = pieces >= 2 * fill ? 2 : 1;
+    const int steps = pieces >= kAdamDeep * fill ? kAdamDeep : 1;
     int i = 0;
     while (i < l.count) {
         AdamTable<kMost> tb;
