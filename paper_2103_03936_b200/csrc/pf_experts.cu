@@ -18,10 +18,11 @@ namespace pf {
 namespace {
 
 // ------------------------------------------------------------------------------ sort
-// One cluster of blocks, each with a contiguous share of the assignments, each of its warps with a contiguous part of that.  A
-// warp takes 32 assignments at a time: lanes that chose the same expert find one another, the first of them moves the warp's
-// counter.  Counting first gives every warp the rows before its own (the warps before it in its block, the blocks
-// before it through distributed shared memory); walking the same assignments again gives each its row.
+// One cluster of blocks, each with a contiguous share of the assignments, each of its warps with a contiguous part of that.  Counting
+// first gives every warp the rows before its own (the warps before it in its block, the blocks before it through distributed shared
+// memory); then a warp walks its assignments in order, 32 at a time: lanes that chose the same expert find one another, the
+// first of them moves the warp's counter.  Bound by latency: a launch, one trip to memory for up to 256 assignments of a warp, which stay
+// in registers, and the cluster's meeting.
 constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32, kSortBlocks = 8;
 constexpr int kMostExperts = 2048;
 
@@ -76,13 +77,21 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const unsigned before = (1u << lane) - 1u;
-    for (int a0 = beg; a0 < end; a0 += 32) {
-        const int a = a0 + lane;
-        int e = a < end ? p.ids[a] : -1;
-        if (e >= E) e = -1;
-        const unsigned same = __match_any_sync(0xffffffffu, e);
-        if (e >= 0 && (same & before) == 0) mine[e] += __popc(same);
-        __syncwarp();
+    constexpr int kHeld = 8;      // assignments of a lane in registers
+    int held[kHeld];
+    auto hold = [&](int a0) {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int a = a0 + 32 * i + lane;
+            held[i] = a < end ? p.ids[a] : -1;
+            if (held[i] >= E) held[i] = -1;
+        }
+    };
+    for (int a0 = beg; a0 < end; a0 += 32 * kHeld) {
+        hold(a0);
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (held[i] >= 0) atomicAdd(mine + held[i], 1);
     }
     __syncthreads();
     for (int e = threadIdx.x; e < E; e += kSortThreads) {
@@ -146,21 +155,24 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) 
     } else {
         for (int r = first[E - 1] + chosen[E - 1] + thread; r < p.rows; r += threads) p.sources[r] = -1;
     }
-    for (int a0 = beg; a0 < end; a0 += 32) {
-        const int a = a0 + lane;
-        int e = a < end ? p.ids[a] : -1;
-        if (e >= E) e = -1;
-        const unsigned same = __match_any_sync(0xffffffffu, e);
-        int r = 0;
-        if (e >= 0) r = mine[e] + __popc(same & before);
-        __syncwarp();
-        if (e >= 0 && (same & before) == 0) mine[e] += __popc(same);
-        __syncwarp();
-        if (a < end) {
-            const bool in = e >= 0 && (p.capacity == 0 || r < p.capacity);
-            const int slot = in ? first[e] + r : -1;
-            p.slots[a] = slot;
-            if (in) p.sources[slot] = a;
+    for (int a0 = beg; a0 < end; a0 += 32 * kHeld) {
+        if (end - beg > 32 * kHeld) hold(a0);
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int a = a0 + 32 * i + lane, e = held[i];
+            if (a0 + 32 * i >= end) break;
+            const unsigned same = __match_any_sync(0xffffffffu, e);
+            int r = 0;
+            if (e >= 0) r = mine[e] + __popc(same & before);
+            __syncwarp();
+            if (e >= 0 && (same & before) == 0) mine[e] += __popc(same);
+            __syncwarp();
+            if (a < end) {
+                const bool in = e >= 0 && (p.capacity == 0 || r < p.capacity);
+                const int slot = in ? first[e] + r : -1;
+                p.slots[a] = slot;
+                if (in) p.sources[slot] = a;
+            }
         }
     }
     cluster_sync();      // (no block leaves while another reads its totals)
@@ -217,172 +229,181 @@ struct RowParams {
     int64_t pitch, in_pitch, out_pitch;      // bytes
     int tokens, k, rows;
     int parts;                // pieces of a row
-    int token_blocks;         // blocks that walk tokens; the others clear rows
 };
 
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
-constexpr int kRowsPerBlock = 32;      // of a block that clears rows
+constexpr int kRowsToClear = 4;      // rows of experts that a warp looks at beside its token
 constexpr int kDispatchDeep = 4, kCombineDeep = 2;      // pieces of a row that a lane has in hand
 
-// Clears the rows among 32 that no token has.
+// Clears those of a warp's rows that no token has, pieces v0, v0 + step, ... of them.
 template <typename T, int kBytes>
-__device__ __forceinline__ void clear_rows(const RowParams& p, int block) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int row = block * kRowsPerBlock + lane;
-    unsigned empty = __ballot_sync(0xffffffffu, row < p.rows && p.sources[row] < 0);
+__device__ __forceinline__ void clear_rows(const RowParams& p, int64_t item, int v0, int step) {
+    const int lane = threadIdx.x & 31;
+    const int64_t first = item * kRowsToClear;
+    if (first >= p.rows) return;
+    const int64_t row = first + lane;
+    unsigned empty = __ballot_sync(0xffffffffu, lane < kRowsToClear && row < p.rows && p.sources[row] < 0);
     Part<T, kBytes> z;
     z.zero();
     for (; empty; empty &= empty - 1) {
-        char* const to = p.rows_out + static_cast<int64_t>(block * kRowsPerBlock + __ffs(empty) - 1) * p.out_pitch;
-        for (int v = warp * 32 + lane; v < p.parts; v += kRowThreads) z.store(to + static_cast<int64_t>(v) * kBytes);
+        char* const to = p.rows_out + (first + __ffs(empty) - 1) * p.out_pitch;
+        for (int v = v0; v < p.parts; v += step) z.store(to + static_cast<int64_t>(v) * kBytes);
     }
 }
 
-// xs[slot] = x[token]: a warp to 32 * kDispatchDeep pieces of a token's row.
+// xs[slot] = x[token]: a warp to a token's row, 32 * kDispatchDeep pieces at a time (gridDim.y warps to long ones).
 template <typename T, int kBytes>
 __global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowParams p) {
     constexpr int kDeep = kDispatchDeep;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int block = static_cast<int>(blockIdx.x);
-    if (block >= p.token_blocks) return clear_rows<T, kBytes>(p, block - p.token_blocks);
     const int lane = threadIdx.x & 31;
-    const int segments = (p.parts + 32 * kDeep - 1) / (32 * kDeep);
-    const int64_t item = static_cast<int64_t>(block) * kRowWarps + (threadIdx.x >> 5);
-    const int64_t token = item / segments;
-    if (token >= p.tokens) return;
-    const int v0 = static_cast<int>(item % segments) * 32 * kDeep + lane;
-    const char* const from = p.x + token * p.pitch;
-    Part<T, kBytes> d[kDeep];
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * kRowWarps + (threadIdx.x >> 5);
+    if (item < p.tokens) {
+        const char* const from = p.x + item * p.pitch;
+        for (int v0 = blockIdx.y * 32 * kDeep + lane; v0 < p.parts; v0 += gridDim.y * 32 * kDeep) {
+            Part<T, kBytes> d[kDeep];
 #pragma unroll
-    for (int u = 0; u < kDeep; ++u)
-        if (v0 + 32 * u < p.parts) d[u].load(from + static_cast<int64_t>(v0 + 32 * u) * kBytes);
-    for (int j = 0; j < p.k; ++j) {
-        const int slot = p.slots[token * p.k + j];
-        if (slot < 0 || slot >= p.rows) continue;
-        char* const to = p.rows_out + static_cast<int64_t>(slot) * p.out_pitch;
+            for (int u = 0; u < kDeep; ++u)
+                if (v0 + 32 * u < p.parts) d[u].load(from + static_cast<int64_t>(v0 + 32 * u) * kBytes);
+            for (int j = 0; j < p.k; ++j) {
+                const int slot = p.slots[item * p.k + j];
+                if (slot < 0 || slot >= p.rows) continue;
+                char* const to = p.rows_out + static_cast<int64_t>(slot) * p.out_pitch;
 #pragma unroll
-        for (int u = 0; u < kDeep; ++u)
-            if (v0 + 32 * u < p.parts) d[u].store(to + static_cast<int64_t>(v0 + 32 * u) * kBytes);
+                for (int u = 0; u < kDeep; ++u)
+                    if (v0 + 32 * u < p.parts) d[u].store(to + static_cast<int64_t>(v0 + 32 * u) * kBytes);
+            }
+        }
     }
+    clear_rows<T, kBytes>(p, item, blockIdx.y * 32 + lane, gridDim.y * 32);
 }
 
-// y[token] = sum_j w_j rows_in[slot_j]: a warp to 32 * kCombineDeep pieces of a token's row.
+// y[token] = sum_j w_j rows_in[slot_j]: a warp to 32 * kCombineDeep pieces of a token's row at a time.
 template <typename T, int kBytes>
 __global__ void __launch_bounds__(kRowThreads) combine_kernel(const RowParams p) {
     constexpr int kDeep = kCombineDeep, kN = Part<T, kBytes>::kN;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31;
-    const int segments = (p.parts + 32 * kDeep - 1) / (32 * kDeep);
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * kRowWarps + (threadIdx.x >> 5);
-    const int64_t token = item / segments;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * kRowWarps + (threadIdx.x >> 5);
     if (token >= p.tokens) return;
-    const int v0 = static_cast<int>(item % segments) * 32 * kDeep + lane;
-    float sum[kDeep][kN];
-#pragma unroll
-    for (int u = 0; u < kDeep; ++u)
-#pragma unroll
-        for (int i = 0; i < kN; ++i) sum[u][i] = 0.f;
-#pragma unroll 2
-    for (int j = 0; j < p.k; ++j) {
-        const int slot = p.slots[token * p.k + j];
-        if (slot < 0 || slot >= p.rows) continue;
-        const float w = p.weights ? p.weights[token * p.k + j] : 1.f;
-        const char* const from = p.rows_in + static_cast<int64_t>(slot) * p.in_pitch;
-        Part<T, kBytes> d[kDeep];
+    for (int v0 = blockIdx.y * 32 * kDeep + lane; v0 < p.parts; v0 += gridDim.y * 32 * kDeep) {
+        float sum[kDeep][kN];
 #pragma unroll
         for (int u = 0; u < kDeep; ++u)
-            if (v0 + 32 * u < p.parts) d[u].load(from + static_cast<int64_t>(v0 + 32 * u) * kBytes);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) sum[u][i] = 0.f;
+#pragma unroll 2
+        for (int j = 0; j < p.k; ++j) {
+            const int slot = p.slots[token * p.k + j];
+            if (slot < 0 || slot >= p.rows) continue;
+            const float w = p.weights ? p.weights[token * p.k + j] : 1.f;
+            const char* const from = p.rows_in + static_cast<int64_t>(slot) * p.in_pitch;
+            Part<T, kBytes> d[kDeep];
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u)
+                if (v0 + 32 * u < p.parts) d[u].load(from + static_cast<int64_t>(v0 + 32 * u) * kBytes);
+#pragma unroll
+            for (int u = 0; u < kDeep; ++u) {
+                if (v0 + 32 * u >= p.parts) continue;
+                float x[kN];
+                d[u].get(x);
+#pragma unroll
+                for (int i = 0; i < kN; ++i) sum[u][i] = fmaf(w, x[i], sum[u][i]);
+            }
+        }
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) {
             if (v0 + 32 * u >= p.parts) continue;
-            float x[kN];
-            d[u].get(x);
-#pragma unroll
-            for (int i = 0; i < kN; ++i) sum[u][i] = fmaf(w, x[i], sum[u][i]);
+            Part<T, kBytes> d;
+            d.set(sum[u]);
+            d.store(p.y + token * p.pitch + static_cast<int64_t>(v0 + 32 * u) * kBytes);
         }
-    }
-#pragma unroll
-    for (int u = 0; u < kDeep; ++u) {
-        if (v0 + 32 * u >= p.parts) continue;
-        Part<T, kBytes> d;
-        d.set(sum[u]);
-        d.store(p.y + token * p.pitch + static_cast<int64_t>(v0 + 32 * u) * kBytes);
     }
 }
 
-// dys[slot] = w dy[token], dw = <dy[token], ys[slot]>: kWide a block to a token, else a warp.
-template <typename T, int kBytes, bool kWide>
+// dys[slot] = w dy[token], dw = <dy[token], ys[slot]> for kGroup experts of a token at a time: kWide a block to a token, else a warp.
+template <typename T, int kBytes, bool kWide, int kGroup>
 __global__ void __launch_bounds__(kRowThreads) combine_bwd_kernel(const RowParams p) {
-    constexpr int kN = Part<T, kBytes>::kN, kGroup = 4;      // experts of a token at a time
+    constexpr int kN = Part<T, kBytes>::kN, kDeep = kGroup == 4 ? 1 : 2;
     constexpr int kStep = kWide ? kRowThreads : 32;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int block = static_cast<int>(blockIdx.x);
-    if (block >= p.token_blocks) return clear_rows<T, kBytes>(p, block - p.token_blocks);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t token = kWide ? block : static_cast<int64_t>(block) * kRowWarps + warp;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * kRowWarps + warp, token = kWide ? blockIdx.x : item;
     __shared__ float red[kWide ? kRowWarps * kGroup : 1];
-    if (token >= p.tokens) return;
-    const char* const dy = p.x + token * p.pitch;
-    for (int j0 = 0; j0 < p.k; j0 += kGroup) {
-        int slot[kGroup];
-        float w[kGroup], dot[kGroup];
-#pragma unroll
-        for (int j = 0; j < kGroup; ++j) {
-            const bool in = j0 + j < p.k;
-            slot[j] = in ? p.slots[token * p.k + j0 + j] : -1;
-            if (slot[j] >= p.rows) slot[j] = -1;
-            w[j] = in ? p.weights[token * p.k + j0 + j] : 0.f;
-            dot[j] = 0.f;
-        }
-        for (int v = (kWide ? static_cast<int>(threadIdx.x) : lane); v < p.parts; v += kStep) {
-            Part<T, kBytes> d, r[kGroup];
-            d.load(dy + static_cast<int64_t>(v) * kBytes);
-#pragma unroll
-            for (int j = 0; j < kGroup; ++j)
-                if (slot[j] >= 0) r[j].load(p.rows_in + slot[j] * p.in_pitch + static_cast<int64_t>(v) * kBytes);
-            float g[kN];
-            d.get(g);
+    if (token < p.tokens) {
+        const char* const dy = p.x + token * p.pitch;
+        for (int j0 = 0; j0 < p.k; j0 += kGroup) {
+            int slot[kGroup];
+            float w[kGroup], dot[kGroup];
 #pragma unroll
             for (int j = 0; j < kGroup; ++j) {
-                if (slot[j] < 0) continue;
-                float x[kN];
-                r[j].get(x);
+                const bool in = j0 + j < p.k;
+                slot[j] = in ? p.slots[token * p.k + j0 + j] : -1;
+                if (slot[j] >= p.rows) slot[j] = -1;
+                w[j] = in ? p.weights[token * p.k + j0 + j] : 0.f;
+                dot[j] = 0.f;
+            }
+            for (int v0 = kWide ? static_cast<int>(threadIdx.x) : lane; v0 < p.parts; v0 += kStep * kDeep) {
+                Part<T, kBytes> d[kDeep], r[kGroup][kDeep];
 #pragma unroll
-                for (int i = 0; i < kN; ++i) {
-                    dot[j] = fmaf(g[i], x[i], dot[j]);
-                    x[i] = g[i] * w[j];
+                for (int u = 0; u < kDeep; ++u) {
+                    const int v = v0 + u * kStep;
+                    if (v >= p.parts) continue;
+                    d[u].load(dy + static_cast<int64_t>(v) * kBytes);
+#pragma unroll
+                    for (int j = 0; j < kGroup; ++j)
+                        if (slot[j] >= 0) r[j][u].load(p.rows_in + slot[j] * p.in_pitch + static_cast<int64_t>(v) * kBytes);
                 }
-                if (p.rows_out) {
-                    r[j].set(x);
-                    r[j].store(p.rows_out + slot[j] * p.out_pitch + static_cast<int64_t>(v) * kBytes);
+#pragma unroll
+                for (int u = 0; u < kDeep; ++u) {
+                    const int v = v0 + u * kStep;
+                    if (v >= p.parts) continue;
+                    float g[kN];
+                    d[u].get(g);
+#pragma unroll
+                    for (int j = 0; j < kGroup; ++j) {
+                        if (slot[j] < 0) continue;
+                        float x[kN];
+                        r[j][u].get(x);
+#pragma unroll
+                        for (int i = 0; i < kN; ++i) {
+                            dot[j] = fmaf(g[i], x[i], dot[j]);
+                            x[i] = g[i] * w[j];
+                        }
+                        if (p.rows_out) {
+                            r[j][u].set(x);
+                            r[j][u].store(p.rows_out + slot[j] * p.out_pitch + static_cast<int64_t>(v) * kBytes);
+                        }
+                    }
                 }
             }
-        }
-        if (!p.dweights) continue;
-#pragma unroll
-        for (int j = 0; j < kGroup; ++j)
-#pragma unroll
-            for (int o = 16; o > 0; o /= 2) dot[j] += __shfl_xor_sync(0xffffffffu, dot[j], o);
-        if constexpr (kWide) {
-            __syncthreads();
-            if (lane == 0)
-#pragma unroll
-                for (int j = 0; j < kGroup; ++j) red[warp * kGroup + j] = dot[j];
-            __syncthreads();
-            if (threadIdx.x < kGroup && j0 + static_cast<int>(threadIdx.x) < p.k) {
-                float s = 0.f;
-                for (int u = 0; u < kRowWarps; ++u) s += red[u * kGroup + threadIdx.x];
-                p.dweights[token * p.k + j0 + threadIdx.x] = s;
-            }
-        } else if (lane == 0) {
+            if (!p.dweights) continue;
 #pragma unroll
             for (int j = 0; j < kGroup; ++j)
-                if (j0 + j < p.k) p.dweights[token * p.k + j0 + j] = dot[j];
+#pragma unroll
+                for (int o = 16; o > 0; o /= 2) dot[j] += __shfl_xor_sync(0xffffffffu, dot[j], o);
+            if constexpr (kWide) {
+                __syncthreads();
+                if (lane == 0)
+#pragma unroll
+                    for (int j = 0; j < kGroup; ++j) red[warp * kGroup + j] = dot[j];
+                __syncthreads();
+                if (threadIdx.x < kGroup && j0 + static_cast<int>(threadIdx.x) < p.k) {
+                    float s = 0.f;
+                    for (int u = 0; u < kRowWarps; ++u) s += red[u * kGroup + threadIdx.x];
+                    p.dweights[token * p.k + j0 + threadIdx.x] = s;
+                }
+            } else if (lane == 0) {
+#pragma unroll
+                for (int j = 0; j < kGroup; ++j)
+                    if (j0 + j < p.k) p.dweights[token * p.k + j0 + j] = dot[j];
+            }
         }
     }
+    if (p.rows_out) clear_rows<T, kBytes>(p, item, lane, 32);
 }
 
 // ------------------------------------------------------------------------------ host side
@@ -410,22 +431,26 @@ int check_sizes(int64_t tokens, int k, int64_t rows, int64_t width, int dtype) {
 
 enum RowOp { kDispatch, kCombine, kCombineBwd };
 template <typename T, int kBytes>
+cudaError_t combine_bwd_run(const RowParams& p, cudaStream_t stream) {
+    // a block to a token where a warp to each would leave most of the machine idle
+    const bool wide = p.tokens < num_sms() * kRowWarps * 2 && p.parts > 32;
+    const int64_t blocks = std::max(wide ? static_cast<int64_t>(p.tokens) : ceil_div(p.tokens, kRowWarps),
+                                    p.rows_out ? ceil_div(p.rows, kRowsToClear * kRowWarps) : 0);
+    if (blocks == 0) return cudaSuccess;
+    const auto kernel = wide ? (p.k == 1 ? combine_bwd_kernel<T, kBytes, true, 1> : p.k == 2 ? combine_bwd_kernel<T, kBytes, true, 2> : combine_bwd_kernel<T, kBytes, true, 4>)
+                             : (p.k == 1 ? combine_bwd_kernel<T, kBytes, false, 1> : p.k == 2 ? combine_bwd_kernel<T, kBytes, false, 2> : combine_bwd_kernel<T, kBytes, false, 4>);
+    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kRowThreads, 0, 1, stream, p);
+}
+template <typename T, int kBytes>
 cudaError_t rows_run(RowOp op, RowParams p, int64_t width, cudaStream_t stream) {
     p.parts = static_cast<int>(width * static_cast<int64_t>(sizeof(T)) / kBytes);
-    const int64_t clear = p.rows_out ? ceil_div(p.rows, kRowsPerBlock) : 0;
-    // (backward of combine) a block to a token where a warp to each would leave most of the machine idle
-    const bool wide = p.tokens < num_sms() * kRowWarps * 2 && p.parts > 32;
-    int64_t blocks = 0;
-    if (op == kDispatch) blocks = ceil_div(p.tokens * ceil_div(p.parts, 32 * kDispatchDeep), kRowWarps);
-    else if (op == kCombine) blocks = ceil_div(p.tokens * ceil_div(p.parts, 32 * kCombineDeep), kRowWarps);
-    else blocks = wide ? p.tokens : ceil_div(p.tokens, kRowWarps);
-    if (blocks + clear == 0) return cudaSuccess;
-    if (blocks + clear > 0x7fffffffLL) return cudaErrorInvalidValue;
-    p.token_blocks = static_cast<int>(blocks);
-    const auto kernel = op == kDispatch ? dispatch_kernel<T, kBytes>
-                        : op == kCombine ? combine_kernel<T, kBytes>
-                        : wide ? combine_bwd_kernel<T, kBytes, true> : combine_bwd_kernel<T, kBytes, false>;
-    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks + clear)), kRowThreads, 0, 1, stream, p);
+    if (op == kCombineBwd) return combine_bwd_run<T, kBytes>(p, stream);
+    const bool dispatch = op == kDispatch;
+    const int64_t segments = std::min<int64_t>(ceil_div(p.parts, 32 * (dispatch ? kDispatchDeep : kCombineDeep)), 65535);
+    const int64_t blocks = std::max(ceil_div(p.tokens, kRowWarps), dispatch ? ceil_div(p.rows, kRowsToClear * kRowWarps) : 0);
+    if (blocks == 0) return cudaSuccess;
+    const auto kernel = dispatch ? dispatch_kernel<T, kBytes> : combine_kernel<T, kBytes>;
+    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(segments)), kRowThreads, 0, 1, stream, p);
 }
 cudaError_t rows_launch(RowOp op, const RowParams& p, int bytes, int64_t width, int dtype, cudaStream_t stream) {
     if (dtype == PF_BF16) {
