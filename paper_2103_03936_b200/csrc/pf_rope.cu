@@ -456,7 +456,8 @@ __global__ void __launch_bounds__(kAnyThreads) rope_any_kernel(const RopeParams 
     }
 }
 
-// dw of both sides: the sums of the blocks, added in block order by eight warps to 32 columns (warp v takes blocks v, v + 8, ...).
+// dw of both sides: the sums of the blocks, added in block order by 32 warps to 32 columns (warp v takes blocks v, v + 32, ...).
+constexpr int kWeightWarps = 32;
 struct WeightSums {
     const float* partial[2];
     void* out[2];
@@ -464,7 +465,7 @@ struct WeightSums {
     int dim, accumulate;
 };
 template <typename T>
-__global__ void __launch_bounds__(256) rope_weight_kernel(const WeightSums p) {
+__global__ void __launch_bounds__(kWeightWarps * 32) rope_weight_kernel(const WeightSums p) {
     const int side = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = static_cast<int>(blockIdx.x) * 32 + lane;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -473,13 +474,13 @@ __global__ void __launch_bounds__(256) rope_weight_kernel(const WeightSums p) {
     float sum = 0.f;
     if (col < p.dim)
 #pragma unroll 8
-        for (int b = warp; b < p.blocks[side]; b += 8) sum += p.partial[side][static_cast<int64_t>(b) * p.dim + col];
-    __shared__ float red[8][32];
+        for (int b = warp; b < p.blocks[side]; b += kWeightWarps) sum += p.partial[side][static_cast<int64_t>(b) * p.dim + col];
+    __shared__ float red[kWeightWarps][32];
     red[warp][lane] = sum;
     __syncthreads();
     if (warp == 0 && col < p.dim) {
 #pragma unroll
-        for (int v = 1; v < 8; ++v) sum += red[v][lane];
+        for (int v = 1; v < kWeightWarps; ++v) sum += red[v][lane];
         put1(out + col, p.accumulate ? get1(out + col) + sum : sum);
     }
 }
@@ -694,7 +695,7 @@ int pf_qk_norm_rope_bwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
     ws.dim = dim;
     ws.accumulate = flags & PF_GRAD_ACCUMULATE ? 1 : 0;
     const auto add = wtype == PF_BF16 ? rope_weight_kernel<__nv_bfloat16> : rope_weight_kernel<float>;
-    PF_CUDA(launch_beside(add, dim3(static_cast<unsigned>(ceil_div(dim, 32)), 2), 256, 0, 1, stream, ws));
+    PF_CUDA(launch_beside(add, dim3(static_cast<unsigned>(ceil_div(dim, 32)), 2), kWeightWarps * 32, 0, 1, stream, ws));
     return PF_OK;
 }
 
