@@ -352,7 +352,8 @@ int pf_unpack_factor_grads(const void* flat, int64_t flat_elems, void* const* gr
  *   sources [rows]        int32  assignment of each row, -1 for none
  *   counts  [experts]     int32  assignments that chose the expert, those without a row among them
  *   offsets [experts + 1] int32  first row of each expert; behind the last, experts * capacity or the rows in use
- * One launch of up to eight blocks, no workspace.  PF_ERR_UNSUPPORTED: more than 2048 experts, or 2^30 assignments or rows.
+ * One launch and no workspace up to 32768 assignments; two launches and pf_expert_sort_workspace bytes beyond.  PF_ERR_UNSUPPORTED: more than
+ * 2048 experts, or 2^30 assignments or rows.
  * pf_expert_rows returns `rows` (0 for invalid sizes).
  *
  * The other four take slots and sources as pf_expert_sort left them (an index outside the rows counts as none) and
@@ -367,8 +368,11 @@ int pf_unpack_factor_grads(const void* flat, int64_t flat_elems, void* const* gr
  * ------------------------------------------------------------------------------- */
 int64_t pf_expert_rows(int64_t tokens, int k, int experts, int64_t capacity);
 
+size_t pf_expert_sort_workspace(int64_t tokens, int k, int experts);
+
 int pf_expert_sort(const int32_t* ids, int64_t tokens, int k, int experts, int64_t capacity,
-                   int32_t* slots, int32_t* sources, int32_t* counts, int32_t* offsets, void* cuda_stream);
+                   int32_t* slots, int32_t* sources, int32_t* counts, int32_t* offsets,
+                   void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 int pf_expert_dispatch_fwd(const void* x, int64_t ldx, const int32_t* slots, const int32_t* sources, void* xs, int64_t ldxs,
                            int64_t tokens, int k, int64_t rows, int64_t width, int dtype, void* cuda_stream);
@@ -445,7 +449,7 @@ int pf_qk_norm_rope_bwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
  * arrays of different tensors must not overlap.
  * scalars: NULL, or a device array (4-byte aligned) that replaces lr, step (by the two corrections), grad_scale and seed, for
  * steps replayed from a CUDA graph.  The library reads it when the step runs.
- * One launch for up to 256 tensors, no workspace. */
+ * One launch for up to 448 tensors, no workspace. */
 typedef enum {
     PF_STATE_F32 = 0,
     PF_STATE_8BIT = 1

@@ -90,7 +90,9 @@ def lib() -> ctypes.CDLL:
         L.pf_expert_rows.restype = i64
         L.pf_expert_rows.argtypes = [i64, ci, ci, i64]
         L.pf_expert_sort.restype = ci
-        L.pf_expert_sort.argtypes = [vp, i64, ci, ci, i64, vp, vp, vp, vp, vp]
+        L.pf_expert_sort.argtypes = [vp, i64, ci, ci, i64, vp, vp, vp, vp, vp, sz, vp]
+        L.pf_expert_sort_workspace.restype = sz
+        L.pf_expert_sort_workspace.argtypes = [i64, ci, ci]
         sizes = [i64, ci, i64, i64, ci, vp]
         L.pf_expert_dispatch_fwd.restype = ci
         L.pf_expert_dispatch_fwd.argtypes = [vp, i64, vp, vp, vp, i64] + sizes
@@ -260,11 +262,15 @@ def pf_expert_rows(tokens, k, experts, capacity=0) -> int:
     return int(lib().pf_expert_rows(tokens, k, experts, capacity))
 
 
-def pf_expert_sort(ids, experts, *, capacity=0, slots=None, sources=None, counts=None, offsets=None, stream=None, prepare=False):
+def pf_expert_sort_workspace(tokens, k, experts) -> int:
+    return int(lib().pf_expert_sort_workspace(tokens, k, experts))
+
+
+def pf_expert_sort(ids, experts, *, capacity=0, slots=None, sources=None, counts=None, offsets=None, workspace=None, stream=None, prepare=False):
     """Rows of a layer's experts for the assignments ids [tokens, k] (int32).  Returns (slots [tokens, k], sources [rows],
     counts [experts], offsets [experts + 1]), all int32; rows = experts * capacity, or tokens * k without a capacity."""
     n = _native or _load_native()
-    return n.expert_sort(ids, experts, capacity, slots, sources, counts, offsets, stream, prepare)
+    return n.expert_sort(ids, experts, capacity, slots, sources, counts, offsets, workspace, stream, prepare)
 
 
 def pf_expert_dispatch_fwd(x, slots, sources, *, xs=None, stream=None, prepare=False):

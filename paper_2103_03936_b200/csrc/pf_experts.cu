@@ -18,15 +18,20 @@ namespace pf {
 namespace {
 
 // ------------------------------------------------------------------------------ sort
-// One cluster of blocks, each with a contiguous share of the assignments, each of its warps with a contiguous part of that.  Counting
-// first gives every warp the rows before its own (the warps before it in its block, the blocks before it through distributed shared
-// memory); then a warp walks its assignments in order, 32 at a time: lanes that chose the same expert find one another, the
-// first of them moves the warp's counter.  Bound by latency: a launch, one trip to memory for up to 256 assignments of a warp, which stay
-// in registers, and the cluster's meeting.
-constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32, kSortBlocks = 8;
+// Blocks with a contiguous share of the assignments each, each of their warps with a contiguous part of that.  Counting first gives every
+// warp the rows before its own (the warps before it in its block, the blocks before it); then a warp walks its assignments in order, 32 at a
+// time: lanes that chose the same expert find one another by ballots, the first of them moves the warp's counter.
+//
+// Up to 32768 assignments: one cluster of up to eight blocks, which read one another's counts from distributed shared memory.  Bound by
+// latency: a launch, a trip to memory for the assignments (which stay in registers), the cluster's meeting.  More of them keep eight SMs busy for
+// too long, with single stores of sources above all (240 000 to 256 experts: 35 us): then a launch counts and a
+// second one sorts, on up to every SM (15.5 us).
+constexpr int kSortBlocks = 8;
 constexpr int kMostExperts = 2048;
+constexpr int64_t kClusterMost = 32768;
 
 struct SortParams {
+    int* totals;      // [blocks, experts]: the blocks' counts, where they are no cluster
     const int* ids;
     int* slots;
     int* sources;
@@ -59,15 +64,49 @@ __device__ __forceinline__ int load_cluster(const int* p, uint32_t rank) {
 
 // Shared memory: warps x experts counters (which become each warp's next row), then for each expert the block's total, the first row
 // and the whole total.
+// The lanes that have the same value of so many bits, a bit at a time (240 000 assignments to 256 experts on eight blocks: 35 us, with __match_any_sync
+// 40).
+__device__ __forceinline__ unsigned same_value(int value, int bits) {
+    unsigned same = 0xffffffffu;
+    for (int b = 0; b < bits; ++b) {
+        const bool set = (value >> b) & 1;
+        const unsigned with = __ballot_sync(0xffffffffu, set);
+        same &= set ? with : ~with;
+    }
+    return same;
+}
+
+// The blocks' counts for a sort by more blocks than a cluster has.
+constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
+__global__ void __launch_bounds__(kSortThreads) count_kernel(const SortParams p) {
+    extern __shared__ int sort_smem[];
+    for (int e = threadIdx.x; e < p.experts; e += kSortThreads) sort_smem[e] = 0;
+    __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int blocks = static_cast<int>(gridDim.x);
+    const int64_t per_block = static_cast<int64_t>((p.assignments + blocks * kSortThreads - 1) / (blocks * kSortThreads)) * kSortThreads;
+    const int64_t beg = blockIdx.x * per_block, end = min(beg + per_block, static_cast<int64_t>(p.assignments));
+#pragma unroll 4
+    for (int64_t a = beg + threadIdx.x; a < end; a += kSortThreads) {
+        const int e = p.ids[a];
+        if (e >= 0 && e < p.experts) atomicAdd(sort_smem + e, 1);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < p.experts; e += kSortThreads) p.totals[static_cast<int64_t>(blockIdx.x) * p.experts + e] = sort_smem[e];
+}
+
+template <bool kCluster>
 __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) {
     extern __shared__ int sort_smem[];
     const int E = p.experts, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int* const mine = sort_smem + warp * E;
-    int* const total = sort_smem + kSortWarps * E;
+    int* const total = sort_smem + kSortWarps * E;      // (kCluster: of this block; else of the blocks before it)
     int* const first = total + E;
     int* const chosen = first + E;
     __shared__ int scan[kSortWarps];
-    const int blocks = static_cast<int>(cluster_size()), rank = static_cast<int>(cluster_rank());
+    const int blocks = kCluster ? static_cast<int>(cluster_size()) : static_cast<int>(gridDim.x);
+    const int rank = kCluster ? static_cast<int>(cluster_rank()) : static_cast<int>(blockIdx.x);
     const int per_warp = (p.assignments + blocks * kSortThreads - 1) / (blocks * kSortThreads) * 32;      // (at most 2^30 assignments)
     const int64_t beg64 = static_cast<int64_t>(rank * kSortWarps + warp) * per_warp;
     const int beg = beg64 < p.assignments ? static_cast<int>(beg64) : p.assignments;
@@ -77,6 +116,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const unsigned before = (1u << lane) - 1u;
+    const int bits = 33 - __clz(E);      // (-1 differs from every expert in the highest of them)
     constexpr int kHeld = 8;      // assignments of a lane in registers
     int held[kHeld];
     auto hold = [&](int a0) {
@@ -101,20 +141,42 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) 
             sort_smem[w * E + e] = sum;
             sum += c;
         }
-        total[e] = sum;
+        if (kCluster) total[e] = sum;
     }
-    cluster_sync();
+    if (kCluster) {
+        cluster_sync();
+    } else {
+        // the blocks' counts, of as many at a time as there are threads for
+        for (int e = threadIdx.x; e < E; e += kSortThreads) total[e] = chosen[e] = 0;
+        __syncthreads();
+        const int wide = min(E, kSortThreads), apart = kSortThreads / wide, part = threadIdx.x / wide;
+        for (int e = threadIdx.x - part * wide; e < E && part < apart; e += wide) {
+            int below = 0, count = 0;
+#pragma unroll 8
+            for (int b = part; b < blocks; b += apart) {
+                const int c = p.totals[static_cast<int64_t>(b) * E + e];
+                if (b < rank) below += c;
+                count += c;
+            }
+            if (below) atomicAdd(total + e, below);
+            if (count) atomicAdd(chosen + e, count);
+        }
+        __syncthreads();
+    }
     // first rows of the experts: every block adds up the whole
     int carry = 0;
     for (int e0 = 0; e0 < E; e0 += kSortThreads) {
         const int e = e0 + threadIdx.x;
         int count = 0, below = 0;      // of all blocks, of those before this one
-        if (e < E) {
+        if (e < E && kCluster) {
             for (int b = 0; b < blocks; ++b) {
                 const int c = load_cluster(total + e, b);
                 if (b < rank) below += c;
                 count += c;
             }
+        } else if (e < E) {
+            below = total[e];
+            count = chosen[e];
         }
         int row = e * p.capacity;
         if (p.capacity == 0) {
@@ -161,7 +223,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) 
         for (int i = 0; i < kHeld; ++i) {
             const int a = a0 + 32 * i + lane, e = held[i];
             if (a0 + 32 * i >= end) break;
-            const unsigned same = __match_any_sync(0xffffffffu, e);
+            const unsigned same = same_value(e, bits);
             int r = 0;
             if (e >= 0) r = mine[e] + __popc(same & before);
             __syncwarp();
@@ -175,7 +237,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) 
             }
         }
     }
-    cluster_sync();      // (no block leaves while another reads its totals)
+    if (kCluster) cluster_sync();      // (no block leaves while another reads its totals)
 }
 
 // ------------------------------------------------------------------------------ rows
@@ -183,21 +245,17 @@ template <int kBytes> struct Raw;
 template <> struct Raw<16> { using T = uint4; };
 template <> struct Raw<8> { using T = uint2; };
 template <> struct Raw<4> { using T = unsigned; };
-template <> struct Raw<2> { using T = unsigned short; };
 
-// A piece of a row: kBytes of elements of T.
+// A piece of a row: kBytes, kN elements of T.
 template <typename T, int kBytes>
 struct Part {
     static constexpr int kN = kBytes / static_cast<int>(sizeof(T));
     union {
         typename Raw<kBytes>::T raw;
         unsigned short half[kBytes / 2];
-        unsigned word[(kBytes + 3) / 4];
+        unsigned word[kBytes / 4];
     };
     __device__ __forceinline__ Part() {}
-    __device__ __forceinline__ void load(const void* p) { raw = *static_cast<const typename Raw<kBytes>::T*>(p); }
-    __device__ __forceinline__ void store(void* p) const { *static_cast<typename Raw<kBytes>::T*>(p) = raw; }
-    __device__ __forceinline__ void zero() { raw = typename Raw<kBytes>::T{}; }
     __device__ __forceinline__ void get(float (&x)[kN]) const {
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
@@ -206,13 +264,61 @@ struct Part {
         }
     }
     __device__ __forceinline__ void set(const float (&x)[kN]) {
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            if constexpr (sizeof(T) == 4) word[i] = __float_as_uint(x[i]);
-            else {
-                const __nv_bfloat16 t = __float2bfloat16_rn(x[i]);
-                half[i] = *reinterpret_cast<const unsigned short*>(&t);
+            for (int i = 0; i < kN; ++i) word[i] = __float_as_uint(x[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kBytes / 4; ++i) {
+                const __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+                word[i] = *reinterpret_cast<const unsigned*>(&t);
             }
+        }
+    }
+};
+
+// Rows in pieces of kUnit bytes (16, 8 or 4), at boundaries of which all rows start and end.  kUnit = 2 (bf16, odd widths and pitches): in
+// pieces of 16 bytes, those of memory that a row (the one that is written, or the one that `frame` names) lies in: the first starts up to 14
+// bytes before the row, the last ends as far behind it.  Such a piece of another row is put together from the aligned words that it
+// lies in, of which only those are read that hold a byte of the row; the ends of a row are written element by element.
+template <typename T, int kUnit>
+struct Rows {
+    static constexpr bool kAligned = kUnit != 2;
+    static constexpr int kBytes = kAligned ? kUnit : 16;
+    using P = Part<T, kBytes>;
+    static __device__ __forceinline__ int lead(const char* frame) { return kAligned ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(frame) & 15); }
+    static __device__ __forceinline__ int pieces(const char* frame, int bytes) { return kAligned ? bytes / kBytes : (lead(frame) + bytes + 15) / 16; }
+    // Byte of the row at which piece v starts.
+    static __device__ __forceinline__ int place(const char* frame, int v) { return v * kBytes - lead(frame); }
+    static __device__ __forceinline__ bool whole(int at, int bytes) { return kAligned || (at >= 0 && at + 16 <= bytes); }
+    static __device__ __forceinline__ bool inside(int at, int i, int bytes) {
+        const int b = at + i * static_cast<int>(sizeof(T));
+        return b >= 0 && b < bytes;
+    }
+    static __device__ __forceinline__ void load(P& d, const char* row, int at, int bytes) {
+        if constexpr (kAligned) {
+            d.raw = *reinterpret_cast<const decltype(d.raw)*>(row + at);
+        } else {
+            const char* const p = row + at;
+            const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 2);
+            const char* const low = p - odd;
+            // (no branch: it would keep the loads of the pieces that differ in it apart)
+            const int beg = -at + odd, end = bytes - at + odd;      // the row's bytes, counted from `low`
+            unsigned w[5];
+#pragma unroll
+            for (int i = 0; i < 5; ++i)
+                w[i] = 4 * i + 4 > beg && 4 * i < end && (i < 4 || odd) ? *reinterpret_cast<const unsigned*>(low + 4 * i) : 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) d.word[i] = __funnelshift_r(w[i], w[i + 1], odd * 8);
+        }
+    }
+    static __device__ __forceinline__ void store(const P& d, char* row, int at, int bytes) {
+        if (whole(at, bytes)) {
+            *reinterpret_cast<decltype(P::raw)*>(row + at) = d.raw;
+        } else {
+#pragma unroll
+            for (int i = 0; i < P::kN; ++i)
+                if (inside(at, i, bytes)) *reinterpret_cast<unsigned short*>(row + at + 2 * i) = d.half[i];
         }
     }
 };
@@ -228,139 +334,196 @@ struct RowParams {
     float* dweights;
     int64_t pitch, in_pitch, out_pitch;      // bytes
     int tokens, k, rows;
-    int parts;                // pieces of a row
+    int bytes;                // of a row
+    int lanes;                // of a warp to a token: 8, 16 or 32
 };
 
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
-constexpr int kRowsToClear = 4;      // rows of experts that a warp looks at beside its token
+constexpr int kRowsToClear = 4;      // rows of experts that the lanes of a token look at besides
 constexpr int kDispatchDeep = 4, kCombineDeep = 2;      // pieces of a row that a lane has in hand
 
-// Clears those of a warp's rows that no token has, pieces v0, v0 + step, ... of them.
-template <typename T, int kBytes>
+// Clears those of four rows that no token has: pieces v0, v0 + step, ... of them.
+template <typename T, int kUnit>
 __device__ __forceinline__ void clear_rows(const RowParams& p, int64_t item, int v0, int step) {
-    const int lane = threadIdx.x & 31;
     const int64_t first = item * kRowsToClear;
-    if (first >= p.rows) return;
-    const int64_t row = first + lane;
-    unsigned empty = __ballot_sync(0xffffffffu, lane < kRowsToClear && row < p.rows && p.sources[row] < 0);
-    Part<T, kBytes> z;
-    z.zero();
-    for (; empty; empty &= empty - 1) {
-        char* const to = p.rows_out + (first + __ffs(empty) - 1) * p.out_pitch;
-        for (int v = v0; v < p.parts; v += step) z.store(to + static_cast<int64_t>(v) * kBytes);
+    bool empty[kRowsToClear];
+#pragma unroll
+    for (int r = 0; r < kRowsToClear; ++r) empty[r] = first + r < p.rows && p.sources[first + r] < 0;
+    using R = Rows<T, kUnit>;
+    typename R::P z;
+#pragma unroll
+    for (int i = 0; i < R::kBytes / 4; ++i) z.word[i] = 0;
+#pragma unroll
+    for (int r = 0; r < kRowsToClear; ++r) {
+        if (!empty[r]) continue;
+        char* const to = p.rows_out + (first + r) * p.out_pitch;
+        const int n = R::pieces(to, p.bytes);
+        for (int v = v0; v < n; v += step) R::store(z, to, R::place(to, v), p.bytes);
     }
 }
 
-// xs[slot] = x[token]: a warp to a token's row, 32 * kDispatchDeep pieces at a time (gridDim.y warps to long ones).
-template <typename T, int kBytes>
+// xs[slot] = x[token], a group of lanes to a token; gridDim.y groups to a long row.
+template <typename T, int kUnit>
 __global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowParams p) {
-    constexpr int kDeep = kDispatchDeep;
+    using R = Rows<T, kUnit>;
+    using P = typename R::P;
+    constexpr int kDeep = R::kAligned ? kDispatchDeep : 2;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & 31;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * kRowWarps + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & (p.lanes - 1), step = gridDim.y * p.lanes * kDeep;
+    const int64_t item = (static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x) / p.lanes;
     if (item < p.tokens) {
         const char* const from = p.x + item * p.pitch;
-        for (int v0 = blockIdx.y * 32 * kDeep + lane; v0 < p.parts; v0 += gridDim.y * 32 * kDeep) {
-            Part<T, kBytes> d[kDeep];
-#pragma unroll
-            for (int u = 0; u < kDeep; ++u)
-                if (v0 + 32 * u < p.parts) d[u].load(from + static_cast<int64_t>(v0 + 32 * u) * kBytes);
-            for (int j = 0; j < p.k; ++j) {
-                const int slot = p.slots[item * p.k + j];
-                if (slot < 0 || slot >= p.rows) continue;
-                char* const to = p.rows_out + static_cast<int64_t>(slot) * p.out_pitch;
+        const int* const slots = p.slots + item * p.k;
+        if constexpr (R::kAligned) {      // read once
+            const int n = p.bytes / R::kBytes;
+            for (int v0 = blockIdx.y * p.lanes * kDeep + lane; v0 < n; v0 += step) {
+                P d[kDeep];
 #pragma unroll
                 for (int u = 0; u < kDeep; ++u)
-                    if (v0 + 32 * u < p.parts) d[u].store(to + static_cast<int64_t>(v0 + 32 * u) * kBytes);
+                    if (v0 + p.lanes * u < n) R::load(d[u], from, (v0 + p.lanes * u) * R::kBytes, p.bytes);
+#pragma unroll 2
+                for (int j = 0; j < p.k; ++j) {
+                    const int slot = slots[j];
+                    if (slot < 0 || slot >= p.rows) continue;
+                    char* const to = p.rows_out + slot * p.out_pitch;
+#pragma unroll
+                    for (int u = 0; u < kDeep; ++u)
+                        if (v0 + p.lanes * u < n) R::store(d[u], to, (v0 + p.lanes * u) * R::kBytes, p.bytes);
+                }
+            }
+        } else {                       // each row that is written has its own pieces
+            for (int j = 0; j < p.k; ++j) {
+                const int slot = slots[j];
+                if (slot < 0 || slot >= p.rows) continue;
+                char* const to = p.rows_out + slot * p.out_pitch;
+                const int n = R::pieces(to, p.bytes);
+                for (int v0 = blockIdx.y * p.lanes * kDeep + lane; v0 < n; v0 += step) {
+                    P d[kDeep];
+#pragma unroll
+                    for (int u = 0; u < kDeep; ++u)
+                        if (v0 + p.lanes * u < n) R::load(d[u], from, R::place(to, v0 + p.lanes * u), p.bytes);
+#pragma unroll
+                    for (int u = 0; u < kDeep; ++u)
+                        if (v0 + p.lanes * u < n) R::store(d[u], to, R::place(to, v0 + p.lanes * u), p.bytes);
+                }
             }
         }
     }
-    clear_rows<T, kBytes>(p, item, blockIdx.y * 32 + lane, gridDim.y * 32);
+    clear_rows<T, kUnit>(p, item, blockIdx.y * p.lanes + lane, gridDim.y * p.lanes);
 }
 
-// y[token] = sum_j w_j rows_in[slot_j]: a warp to 32 * kCombineDeep pieces of a token's row at a time.
-template <typename T, int kBytes>
+// y[token] = sum_j w_j rows_in[slot_j], kGroup experts of a token at a time.
+template <typename T, int kUnit, int kGroup>
 __global__ void __launch_bounds__(kRowThreads) combine_kernel(const RowParams p) {
-    constexpr int kDeep = kCombineDeep, kN = Part<T, kBytes>::kN;
+    using R = Rows<T, kUnit>;
+    using P = typename R::P;
+    constexpr int kDeep = kCombineDeep, kN = P::kN;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & 31;
-    const int64_t token = static_cast<int64_t>(blockIdx.x) * kRowWarps + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & (p.lanes - 1);
+    const int64_t token = (static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x) / p.lanes;
     if (token >= p.tokens) return;
-    for (int v0 = blockIdx.y * 32 * kDeep + lane; v0 < p.parts; v0 += gridDim.y * 32 * kDeep) {
+    char* const y = p.y + token * p.pitch;
+    const int n = R::pieces(y, p.bytes);
+    for (int v0 = blockIdx.y * p.lanes * kDeep + lane; v0 < n; v0 += gridDim.y * p.lanes * kDeep) {
         float sum[kDeep][kN];
 #pragma unroll
         for (int u = 0; u < kDeep; ++u)
 #pragma unroll
             for (int i = 0; i < kN; ++i) sum[u][i] = 0.f;
-#pragma unroll 2
-        for (int j = 0; j < p.k; ++j) {
-            const int slot = p.slots[token * p.k + j];
-            if (slot < 0 || slot >= p.rows) continue;
-            const float w = p.weights ? p.weights[token * p.k + j] : 1.f;
-            const char* const from = p.rows_in + static_cast<int64_t>(slot) * p.in_pitch;
-            Part<T, kBytes> d[kDeep];
+        for (int j0 = 0; j0 < p.k; j0 += kGroup) {
+            int slot[kGroup];
+            float w[kGroup];
+            P d[kGroup][kDeep];
 #pragma unroll
-            for (int u = 0; u < kDeep; ++u)
-                if (v0 + 32 * u < p.parts) d[u].load(from + static_cast<int64_t>(v0 + 32 * u) * kBytes);
+            for (int j = 0; j < kGroup; ++j) {
+                slot[j] = j0 + j < p.k ? p.slots[token * p.k + j0 + j] : -1;
+                if (slot[j] >= p.rows) slot[j] = -1;
+                w[j] = p.weights && j0 + j < p.k ? p.weights[token * p.k + j0 + j] : 1.f;
+            }
 #pragma unroll
-            for (int u = 0; u < kDeep; ++u) {
-                if (v0 + 32 * u >= p.parts) continue;
-                float x[kN];
-                d[u].get(x);
+            for (int j = 0; j < kGroup; ++j) {
+                if (slot[j] < 0) continue;
+                const char* const from = p.rows_in + slot[j] * p.in_pitch;
 #pragma unroll
-                for (int i = 0; i < kN; ++i) sum[u][i] = fmaf(w, x[i], sum[u][i]);
+                for (int u = 0; u < kDeep; ++u)
+                    if (v0 + p.lanes * u < n) R::load(d[j][u], from, R::place(y, v0 + p.lanes * u), p.bytes);
+            }
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) {
+                if (slot[j] < 0) continue;
+#pragma unroll
+                for (int u = 0; u < kDeep; ++u) {
+                    if (v0 + p.lanes * u >= n) continue;
+                    float x[kN];
+                    d[j][u].get(x);
+#pragma unroll
+                    for (int i = 0; i < kN; ++i) sum[u][i] = fmaf(w[j], x[i], sum[u][i]);
+                }
             }
         }
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) {
-            if (v0 + 32 * u >= p.parts) continue;
-            Part<T, kBytes> d;
+            if (v0 + p.lanes * u >= n) continue;
+            P d;
             d.set(sum[u]);
-            d.store(p.y + token * p.pitch + static_cast<int64_t>(v0 + 32 * u) * kBytes);
+            R::store(d, y, R::place(y, v0 + p.lanes * u), p.bytes);
         }
     }
 }
 
-// dys[slot] = w dy[token], dw = <dy[token], ys[slot]> for kGroup experts of a token at a time: kWide a block to a token, else a warp.
-template <typename T, int kBytes, bool kWide, int kGroup>
+// dys[slot] = w dy[token], dw = <dy[token], ys[slot]> for kGroup experts of a token at a time (one by one where each row has its own pieces): kWide a block
+// to a token, else a group of lanes.
+template <typename T, int kUnit, bool kWide, int kGroup>
 __global__ void __launch_bounds__(kRowThreads) combine_bwd_kernel(const RowParams p) {
-    constexpr int kN = Part<T, kBytes>::kN, kDeep = kGroup == 4 ? 1 : 2;
-    constexpr int kStep = kWide ? kRowThreads : 32;
+    using R = Rows<T, kUnit>;
+    using P = typename R::P;
+    constexpr int kN = P::kN, kDeep = kGroup == 4 ? 1 : 2;
+    static_assert(R::kAligned || kGroup == 1, "");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * kRowWarps + warp, token = kWide ? blockIdx.x : item;
+    const int lanes = kWide ? 32 : p.lanes, lane = threadIdx.x & (lanes - 1), warp = threadIdx.x >> 5;
+    const int64_t item = (static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x) / lanes, token = kWide ? blockIdx.x : item;
+    const int start = kWide ? static_cast<int>(threadIdx.x) : lane, step = kWide ? kRowThreads : lanes;
     __shared__ float red[kWide ? kRowWarps * kGroup : 1];
-    if (token < p.tokens) {
+    if (kWide ? token < p.tokens : __any_sync(0xffffffffu, token < p.tokens)) {      // (all lanes of a warp take part in the sums)
+        const bool there = token < p.tokens;
         const char* const dy = p.x + token * p.pitch;
         for (int j0 = 0; j0 < p.k; j0 += kGroup) {
             int slot[kGroup];
             float w[kGroup], dot[kGroup];
 #pragma unroll
             for (int j = 0; j < kGroup; ++j) {
-                const bool in = j0 + j < p.k;
+                const bool in = there && j0 + j < p.k;
                 slot[j] = in ? p.slots[token * p.k + j0 + j] : -1;
                 if (slot[j] >= p.rows) slot[j] = -1;
                 w[j] = in ? p.weights[token * p.k + j0 + j] : 0.f;
                 dot[j] = 0.f;
             }
-            for (int v0 = kWide ? static_cast<int>(threadIdx.x) : lane; v0 < p.parts; v0 += kStep * kDeep) {
-                Part<T, kBytes> d[kDeep], r[kGroup][kDeep];
+            // the pieces are those of the row that is written, or read where none is
+            const char* frame = dy;
+            if (!R::kAligned && slot[0] >= 0) frame = p.rows_out ? p.rows_out + slot[0] * p.out_pitch : p.rows_in + slot[0] * p.in_pitch;
+            bool any = false;
+#pragma unroll
+            for (int j = 0; j < kGroup; ++j) any = any || slot[j] >= 0;
+            const int n = any ? R::pieces(frame, p.bytes) : 0;
+            for (int v0 = start; v0 < n; v0 += step * kDeep) {
+                P d[kDeep], r[kGroup][kDeep];
 #pragma unroll
                 for (int u = 0; u < kDeep; ++u) {
-                    const int v = v0 + u * kStep;
-                    if (v >= p.parts) continue;
-                    d[u].load(dy + static_cast<int64_t>(v) * kBytes);
+                    const int v = v0 + u * step;
+                    if (v >= n) continue;
+                    R::load(d[u], dy, R::place(frame, v), p.bytes);
 #pragma unroll
                     for (int j = 0; j < kGroup; ++j)
-                        if (slot[j] >= 0) r[j][u].load(p.rows_in + slot[j] * p.in_pitch + static_cast<int64_t>(v) * kBytes);
+                        if (slot[j] >= 0) R::load(r[j][u], p.rows_in + slot[j] * p.in_pitch, R::place(frame, v), p.bytes);
                 }
 #pragma unroll
                 for (int u = 0; u < kDeep; ++u) {
-                    const int v = v0 + u * kStep;
-                    if (v >= p.parts) continue;
+                    const int v = v0 + u * step;
+                    if (v >= n) continue;
+                    const int at = R::place(frame, v);
                     float g[kN];
                     d[u].get(g);
 #pragma unroll
@@ -368,6 +531,11 @@ __global__ void __launch_bounds__(kRowThreads) combine_bwd_kernel(const RowParam
                         if (slot[j] < 0) continue;
                         float x[kN];
                         r[j][u].get(x);
+                        if (!R::whole(at, p.bytes)) {      // what lies beside the row is not part of the sum
+#pragma unroll
+                            for (int i = 0; i < kN; ++i)
+                                if (!R::inside(at, i, p.bytes)) g[i] = x[i] = 0.f;
+                        }
 #pragma unroll
                         for (int i = 0; i < kN; ++i) {
                             dot[j] = fmaf(g[i], x[i], dot[j]);
@@ -375,7 +543,7 @@ __global__ void __launch_bounds__(kRowThreads) combine_bwd_kernel(const RowParam
                         }
                         if (p.rows_out) {
                             r[j][u].set(x);
-                            r[j][u].store(p.rows_out + slot[j] * p.out_pitch + static_cast<int64_t>(v) * kBytes);
+                            R::store(r[j][u], p.rows_out + slot[j] * p.out_pitch, at, p.bytes);
                         }
                     }
                 }
@@ -383,8 +551,7 @@ __global__ void __launch_bounds__(kRowThreads) combine_bwd_kernel(const RowParam
             if (!p.dweights) continue;
 #pragma unroll
             for (int j = 0; j < kGroup; ++j)
-#pragma unroll
-                for (int o = 16; o > 0; o /= 2) dot[j] += __shfl_xor_sync(0xffffffffu, dot[j], o);
+                for (int o = lanes / 2; o > 0; o /= 2) dot[j] += __shfl_xor_sync(0xffffffffu, dot[j], o);
             if constexpr (kWide) {
                 __syncthreads();
                 if (lane == 0)
@@ -396,14 +563,14 @@ __global__ void __launch_bounds__(kRowThreads) combine_bwd_kernel(const RowParam
                     for (int u = 0; u < kRowWarps; ++u) s += red[u * kGroup + threadIdx.x];
                     p.dweights[token * p.k + j0 + threadIdx.x] = s;
                 }
-            } else if (lane == 0) {
+            } else if (there && lane == 0) {
 #pragma unroll
                 for (int j = 0; j < kGroup; ++j)
                     if (j0 + j < p.k) p.dweights[token * p.k + j0 + j] = dot[j];
             }
         }
     }
-    if (p.rows_out) clear_rows<T, kBytes>(p, item, lane, 32);
+    if (p.rows_out) clear_rows<T, kUnit>(p, item, lane, lanes);
 }
 
 // ------------------------------------------------------------------------------ host side
@@ -415,8 +582,8 @@ bool matrix_valid(const Matrix& m, int64_t rows, int64_t width, int dtype) {
     return rows == 0 || (m.p && elem_aligned(m.p, dtype) && m.ld >= width && m.ld < (1LL << 40));
 }
 bool list_valid(const void* p, int64_t n) { return n == 0 || (p && reinterpret_cast<uintptr_t>(p) % 4 == 0); }
-// Bytes of the pieces that rows of all these matrices divide into.
-int piece_bytes(std::initializer_list<Matrix> all, int64_t width, int dtype) {
+// The bytes at a multiple of which the rows of all these matrices start and end, 16 at most.
+int rows_unit(std::initializer_list<Matrix> all, int64_t width, int dtype) {
     const int64_t s = static_cast<int64_t>(dtype_size(dtype));
     uint64_t bits = static_cast<uint64_t>(width * s) | 16;
     for (const Matrix& m : all)
@@ -429,42 +596,55 @@ int check_sizes(int64_t tokens, int k, int64_t rows, int64_t width, int dtype) {
     return PF_OK;
 }
 
+// Blocks of a sort: a cluster's (1, 2, 4 or 8), or more of them.
+int sort_blocks(int64_t assignments) {
+    if (assignments > kClusterMost) return static_cast<int>(std::max<int64_t>(kSortBlocks + 1, std::min<int64_t>(num_sms(), ceil_div(assignments, 4 * kSortThreads))));
+    int blocks = 1;
+    while (blocks < kSortBlocks && static_cast<int64_t>(blocks) * kSortThreads < assignments) blocks *= 2;
+    return blocks;
+}
+
 enum RowOp { kDispatch, kCombine, kCombineBwd };
-template <typename T, int kBytes>
-cudaError_t combine_bwd_run(const RowParams& p, cudaStream_t stream) {
-    // a block to a token where a warp to each would leave most of the machine idle
-    const bool wide = p.tokens < num_sms() * kRowWarps * 2 && p.parts > 32;
-    const int64_t blocks = std::max(wide ? static_cast<int64_t>(p.tokens) : ceil_div(p.tokens, kRowWarps),
-                                    p.rows_out ? ceil_div(p.rows, kRowsToClear * kRowWarps) : 0);
+template <typename T, int kUnit>
+cudaError_t rows_run(RowOp op, RowParams p, cudaStream_t stream) {
+    constexpr bool kAligned = Rows<T, kUnit>::kAligned;
+    const int pieces = p.bytes / Rows<T, kUnit>::kBytes + (kAligned ? 0 : 1);
+    p.lanes = pieces <= 8 ? 8 : pieces <= 16 ? 16 : 32;
+    // (backward of combine) a block to a token where a warp to each would leave most of the machine idle
+    const bool wide = op == kCombineBwd && p.tokens < num_sms() * kRowWarps * 2 && pieces > 32;
+    const int per_block = kRowThreads / p.lanes;
+    int64_t blocks = wide ? static_cast<int64_t>(p.tokens) : ceil_div(p.tokens, per_block), segments = 1;
+    if (p.rows_out) blocks = std::max(blocks, ceil_div(p.rows, static_cast<int64_t>(kRowsToClear) * per_block));
     if (blocks == 0) return cudaSuccess;
-    const auto kernel = wide ? (p.k == 1 ? combine_bwd_kernel<T, kBytes, true, 1> : p.k == 2 ? combine_bwd_kernel<T, kBytes, true, 2> : combine_bwd_kernel<T, kBytes, true, 4>)
-                             : (p.k == 1 ? combine_bwd_kernel<T, kBytes, false, 1> : p.k == 2 ? combine_bwd_kernel<T, kBytes, false, 2> : combine_bwd_kernel<T, kBytes, false, 4>);
-    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kRowThreads, 0, 1, stream, p);
+    void (*kernel)(RowParams) = nullptr;
+    if (op == kDispatch) {
+        kernel = dispatch_kernel<T, kUnit>;
+        segments = ceil_div(pieces, 32 * kDispatchDeep);
+    } else if (op == kCombine) {
+        kernel = p.k == 1 ? combine_kernel<T, kUnit, 1> : p.k == 2 ? combine_kernel<T, kUnit, 2> : combine_kernel<T, kUnit, 4>;
+        segments = ceil_div(pieces, 32 * kCombineDeep);
+    } else if constexpr (kAligned) {
+        kernel = wide ? (p.k == 1 ? combine_bwd_kernel<T, kUnit, true, 1> : p.k == 2 ? combine_bwd_kernel<T, kUnit, true, 2> : combine_bwd_kernel<T, kUnit, true, 4>)
+                      : (p.k == 1 ? combine_bwd_kernel<T, kUnit, false, 1> : p.k == 2 ? combine_bwd_kernel<T, kUnit, false, 2> : combine_bwd_kernel<T, kUnit, false, 4>);
+    } else {
+        kernel = wide ? combine_bwd_kernel<T, kUnit, true, 1> : combine_bwd_kernel<T, kUnit, false, 1>;
+    }
+    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(std::min<int64_t>(segments, 65535))), kRowThreads, 0, 1, stream, p);
 }
-template <typename T, int kBytes>
-cudaError_t rows_run(RowOp op, RowParams p, int64_t width, cudaStream_t stream) {
-    p.parts = static_cast<int>(width * static_cast<int64_t>(sizeof(T)) / kBytes);
-    if (op == kCombineBwd) return combine_bwd_run<T, kBytes>(p, stream);
-    const bool dispatch = op == kDispatch;
-    const int64_t segments = std::min<int64_t>(ceil_div(p.parts, 32 * (dispatch ? kDispatchDeep : kCombineDeep)), 65535);
-    const int64_t blocks = std::max(ceil_div(p.tokens, kRowWarps), dispatch ? ceil_div(p.rows, kRowsToClear * kRowWarps) : 0);
-    if (blocks == 0) return cudaSuccess;
-    const auto kernel = dispatch ? dispatch_kernel<T, kBytes> : combine_kernel<T, kBytes>;
-    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(segments)), kRowThreads, 0, 1, stream, p);
-}
-cudaError_t rows_launch(RowOp op, const RowParams& p, int bytes, int64_t width, int dtype, cudaStream_t stream) {
+cudaError_t rows_launch(RowOp op, RowParams p, int unit, int64_t width, int dtype, cudaStream_t stream) {
+    p.bytes = static_cast<int>(width * static_cast<int64_t>(dtype_size(dtype)));
     if (dtype == PF_BF16) {
-        switch (bytes) {
-            case 16: return rows_run<__nv_bfloat16, 16>(op, p, width, stream);
-            case 8: return rows_run<__nv_bfloat16, 8>(op, p, width, stream);
-            case 4: return rows_run<__nv_bfloat16, 4>(op, p, width, stream);
-            default: return rows_run<__nv_bfloat16, 2>(op, p, width, stream);
+        switch (unit) {
+            case 16: return rows_run<__nv_bfloat16, 16>(op, p, stream);
+            case 8: return rows_run<__nv_bfloat16, 8>(op, p, stream);
+            case 4: return rows_run<__nv_bfloat16, 4>(op, p, stream);
+            default: return rows_run<__nv_bfloat16, 2>(op, p, stream);
         }
     }
-    switch (bytes) {
-        case 16: return rows_run<float, 16>(op, p, width, stream);
-        case 8: return rows_run<float, 8>(op, p, width, stream);
-        default: return rows_run<float, 4>(op, p, width, stream);
+    switch (unit) {
+        case 16: return rows_run<float, 16>(op, p, stream);
+        case 8: return rows_run<float, 8>(op, p, stream);
+        default: return rows_run<float, 4>(op, p, stream);
     }
 }
 
@@ -480,21 +660,32 @@ int64_t pf_expert_rows(int64_t tokens, int k, int experts, int64_t capacity) {
     return capacity > 0 ? experts * capacity : tokens * k;
 }
 
+size_t pf_expert_sort_workspace(int64_t tokens, int k, int experts) {
+    if (tokens < 0 || k < 1 || experts < 1 || k > (1 << 16) || tokens > (1LL << 30) / k || experts > kMostExperts) return 0;
+    const int blocks = sort_blocks(tokens * k);
+    return blocks > kSortBlocks ? align_up(sizeof(int) * static_cast<size_t>(blocks) * experts, 256) : 0;
+}
+
 int pf_expert_sort(const int32_t* ids, int64_t tokens, int k, int experts, int64_t capacity, int32_t* slots, int32_t* sources, int32_t* counts,
-                   int32_t* offsets, void* cuda_stream) {
+                   int32_t* offsets, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     if (tokens < 0 || k < 1 || experts < 1 || capacity < 0) return PF_ERR_INVALID_ARG;
     if (k > (1 << 16) || tokens > (1LL << 30) / k || experts > kMostExperts || capacity > (1LL << 30) / experts) return PF_ERR_UNSUPPORTED;
     const int64_t a = tokens * k, rows = pf_expert_rows(tokens, k, experts, capacity);
     if (!list_valid(ids, a) || !list_valid(slots, a) || !list_valid(sources, rows) || !list_valid(counts, 1) || !list_valid(offsets, 1))
         return PF_ERR_INVALID_ARG;
-    const SortParams p{ids, slots, sources, counts, offsets, static_cast<int>(a), experts, static_cast<int>(capacity), static_cast<int>(rows)};
-    const size_t smem = sizeof(int) * static_cast<size_t>(experts) * (kSortWarps + 3);      // 152 KB for the most experts
-    static std::atomic<uint64_t> allowed{0};
-    if (smem > 48 * 1024)
-        PF_CUDA(allow_dynamic_smem(reinterpret_cast<const void*>(&sort_kernel), sizeof(int) * kMostExperts * (kSortWarps + 3), allowed));
-    int blocks = 1;
-    while (blocks < kSortBlocks && static_cast<int64_t>(blocks) * kSortThreads < a) blocks *= 2;
-    PF_CUDA(launch_beside(sort_kernel, dim3(static_cast<unsigned>(blocks)), kSortThreads, smem, blocks, static_cast<cudaStream_t>(cuda_stream), p));
+    const int st = check_ws(workspace, workspace_bytes, pf_expert_sort_workspace(tokens, k, experts));
+    if (st != PF_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const SortParams p{static_cast<int*>(workspace), ids, slots, sources, counts, offsets, static_cast<int>(a), experts, static_cast<int>(capacity), static_cast<int>(rows)};
+    const int blocks = sort_blocks(a);
+    const bool cluster = blocks <= kSortBlocks;
+    const auto kernel = cluster ? sort_kernel<true> : sort_kernel<false>;
+    const size_t each = sizeof(int) * (kSortWarps + 3);      // of shared memory for an expert: 152 KB for the most of them
+    static std::atomic<uint64_t> allowed[2];
+    if (each * experts > 48 * 1024) PF_CUDA(allow_dynamic_smem(reinterpret_cast<const void*>(kernel), each * kMostExperts, allowed[cluster ? 1 : 0]));
+    const dim3 grid(static_cast<unsigned>(blocks));
+    if (!cluster) PF_CUDA(launch_beside(count_kernel, grid, kSortThreads, sizeof(int) * experts, 1, stream, p));
+    PF_CUDA(launch_beside(kernel, grid, kSortThreads, each * experts, cluster ? blocks : 1, stream, p));
     return PF_OK;
 }
 
@@ -516,7 +707,7 @@ int pf_expert_dispatch_fwd(const void* x, int64_t ldx, const int32_t* slots, con
     p.tokens = static_cast<int>(tokens);
     p.k = k;
     p.rows = static_cast<int>(rows);
-    PF_CUDA(rows_launch(kDispatch, p, piece_bytes({{tokens ? x : nullptr, ldx}, {xs, ldxs}}, width, dtype), width, dtype, static_cast<cudaStream_t>(cuda_stream)));
+    PF_CUDA(rows_launch(kDispatch, p, rows_unit({{tokens ? x : nullptr, ldx}, {xs, ldxs}}, width, dtype), width, dtype, static_cast<cudaStream_t>(cuda_stream)));
     return PF_OK;
 }
 
@@ -538,7 +729,7 @@ int pf_expert_combine_fwd(const void* ys, int64_t ldys, const int32_t* slots, co
     p.tokens = static_cast<int>(tokens);
     p.k = k;
     p.rows = static_cast<int>(rows);
-    PF_CUDA(rows_launch(kCombine, p, piece_bytes({{rows ? ys : nullptr, ldys}, {y, ldy}}, width, dtype), width, dtype, static_cast<cudaStream_t>(cuda_stream)));
+    PF_CUDA(rows_launch(kCombine, p, rows_unit({{rows ? ys : nullptr, ldys}, {y, ldy}}, width, dtype), width, dtype, static_cast<cudaStream_t>(cuda_stream)));
     return PF_OK;
 }
 
@@ -572,7 +763,7 @@ int pf_expert_combine_bwd(const void* ys, int64_t ldys, const int32_t* slots, co
     p.tokens = static_cast<int>(tokens);
     p.k = k;
     p.rows = static_cast<int>(rows);
-    PF_CUDA(rows_launch(kCombineBwd, p, piece_bytes({{rows ? ys : nullptr, ldys}, {tokens ? dy : nullptr, lddy}, {p.rows_out, lddys}}, width, dtype), width,
+    PF_CUDA(rows_launch(kCombineBwd, p, rows_unit({{rows ? ys : nullptr, ldys}, {tokens ? dy : nullptr, lddy}, {p.rows_out, lddys}}, width, dtype), width,
                         dtype, static_cast<cudaStream_t>(cuda_stream)));
     return PF_OK;
 }

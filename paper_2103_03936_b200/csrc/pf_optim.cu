@@ -1,4 +1,4 @@
-// AdamW over a list of tensors: the step that follows the exchange of the flat gradient buffer, in one launch for up to 256 tensors.
+// AdamW over a list of tensors: the step that follows the exchange of the flat gradient buffer, in one launch for up to 448 tensors.
 //
 //   g = grad_scale * grad          m <- beta1 m + (1 - beta1) g          v <- beta2 v + (1 - beta2) g^2
 //   p <- p - lr (weight_decay p + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
@@ -53,7 +53,7 @@ struct AdamTable {
     signed char head[kMost];      // elements in front of the first one at which every array is at a 16-byte boundary
     int first, count;             // place of tensor 0 in the caller's list
     int steps;
-    unsigned char start[kAdamStarts];      // the tensor of chunk i << start_shift
+    unsigned short start[kAdamStarts];      // the tensor of chunk i << start_shift
     int start_shift;
 };
 
@@ -562,7 +562,7 @@ cudaError_t adamw_by(const AdamList& l, const AdamHyper& h, cudaStream_t stream)
         while ((blocks - 1) >> tb.start_shift >= kAdamStarts) ++tb.start_shift;
         for (int c = 0, t = 0; c < blocks; c += 1 << tb.start_shift) {
             while (tb.chunk_prefix[t + 1] <= c) ++t;
-            tb.start[c >> tb.start_shift] = static_cast<unsigned char>(t);
+            tb.start[c >> tb.start_shift] = static_cast<unsigned short>(t);
             if (c > 0x7fffffff - (1 << tb.start_shift)) break;
         }
         const auto kernel = l.state8 ? adamw8_kernel<kMost, kParam, G> : adamw_kernel<kMost, kParam, G>;
@@ -573,9 +573,10 @@ cudaError_t adamw_by(const AdamList& l, const AdamHyper& h, cudaStream_t stream)
 }
 template <int kParam, typename G>
 cudaError_t adamw_sized(const AdamList& l, const AdamHyper& h, cudaStream_t stream) {
-    // (short lists have a table of their own, as in pf_pack.cu: a launch copies all of it)
+    // (short lists have tables of their own, as in pf_pack.cu: a launch copies all of it, 31 KB for 448 tensors)
     if (l.count <= 16) return adamw_by<16, kParam, G>(l, h, stream);
-    return adamw_by<256, kParam, G>(l, h, stream);
+    if (l.count <= 96) return adamw_by<96, kParam, G>(l, h, stream);
+    return adamw_by<448, kParam, G>(l, h, stream);
 }
 template <int kParam>
 cudaError_t adamw_graded(const AdamList& l, const AdamHyper& h, cudaStream_t stream) {

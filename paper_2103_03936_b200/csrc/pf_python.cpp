@@ -725,7 +725,7 @@ int64_t matrix(const OnDevice& on, const at::Tensor& t, const char* name, at::Sc
     return pitch(t, name);
 }
 
-// 0 ids, 1 experts, 2 capacity, 3 slots, 4 sources, 5 counts, 6 offsets, 7 stream, 8 prepare
+// 0 ids, 1 experts, 2 capacity, 3 slots, 4 sources, 5 counts, 6 offsets, 7 workspace, 8 stream, 9 prepare
 PyObject* expert_sort(PyObject* const* a) {
     const at::Tensor& ids = tensor(a[0], "ids");
     const OnDevice on(ids, "ids");
@@ -748,14 +748,17 @@ PyObject* expert_sort(PyObject* const* a) {
     on.check(offsets, "offsets", at::kInt, 1, true);
     expect(slots.sizes() == ids.sizes() && sources.size(0) == rows && counts.size(0) == experts && offsets.size(0) == experts + 1,
            "slots must be as ids, sources [rows], counts [experts], offsets [experts + 1]");
-    const Stream st = stream_of(a[7]);
-    auto f = [=, pi = ints(ids), ps = ints(slots), pr = ints(sources), pc = ints(counts), po = ints(offsets), s = st.s] {
-        return pf_expert_sort(pi, tokens, k, experts, capacity, ps, pr, pc, po, s);
+    const Stream st = stream_of(a[8]);
+    const size_t need = a[7] == Py_None ? pf_expert_sort_workspace(tokens, k, experts) : 0;
+    Workspace ws;
+    if (need > 0 || a[7] != Py_None) ws = workspace(a[7], need, ids, st);
+    auto f = [=, pi = ints(ids), ps = ints(slots), pr = ints(sources), pc = ints(counts), po = ints(offsets), wp = ws.p, wb = ws.bytes, s = st.s] {
+        return pf_expert_sort(pi, tokens, k, experts, capacity, ps, pr, pc, po, wp, wb, s);
     };
-    const bool prepare = truth(a[8]);
+    const bool prepare = truth(a[9]);
     std::vector<at::Tensor> keep;
     if (prepare) keep = {ids, slots, sources, counts, offsets};
-    return issue_on(on, prepare, f, "pf_expert_sort", Workspace(), std::move(keep), tuple({slots, sources, counts, offsets}));
+    return issue_on(on, prepare, f, "pf_expert_sort", std::move(ws), std::move(keep), tuple({slots, sources, counts, offsets}));
 }
 
 struct Choice {
@@ -940,7 +943,7 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 PyMethodDef g_methods[] = {PF_ENTRY(linear_fwd, 12), PF_ENTRY(linear_fwd_static, 6), PF_ENTRY(linear_bwd, 14), PF_ENTRY(bias_act_bwd, 7),
                            PF_ENTRY(grouped_fwd, 9), PF_ENTRY(grouped_bwd, 12), PF_ENTRY(conv_fwd, 11), PF_ENTRY(conv_bwd, 16),
                            PF_ENTRY(pack, 4), PF_ENTRY(unpack, 3), PF_ENTRY(qk_fwd, 12), PF_ENTRY(qk_bwd, 20),
-                           PF_ENTRY(expert_sort, 9), PF_ENTRY(expert_dispatch_fwd, 6), PF_ENTRY(expert_combine_fwd, 7), PF_ENTRY(expert_combine_bwd, 11),
+                           PF_ENTRY(expert_sort, 10), PF_ENTRY(expert_dispatch_fwd, 6), PF_ENTRY(expert_combine_fwd, 7), PF_ENTRY(expert_combine_bwd, 11),
                            PF_ENTRY(adamw_step, 18), {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_pf_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

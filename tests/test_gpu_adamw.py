@@ -90,7 +90,7 @@ def test_many_tensors_span_several_launches():
     t, checks = lists(sizes, torch.float32, torch.float32, False, 0, 0, 2)
     old, before = clones(t), pf.pf_launch_count()
     pf.pf_adamw_step(**t, **H)
-    assert pf.pf_launch_count() - before == 3
+    assert pf.pf_launch_count() - before == 2
     checks[0]()
     for name in ("params", "m", "v"):
         got = torch.cat(t[name])
@@ -146,7 +146,7 @@ def test_8bit_states(pdt, gdt, masters, gap, shift):
 
 def test_8bit_states_from_zero():
     """The first step from zeroed codes and scales, in a list that spans several launches (a tensor's place counts in the whole list)."""
-    sizes = [300 + i % 7 for i in range(300)]
+    sizes = [300 + i % 7 for i in range(500)]
     t, _ = state8(sizes, torch.float32, torch.float32, False, "own", 0, 3)
     for name in ("m", "v", "m_scales", "v_scales"):
         for s in t[name]:

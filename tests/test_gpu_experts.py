@@ -42,7 +42,8 @@ def sorted_rows(ids, experts, capacity):
 
 @pytest.mark.parametrize("tokens,k,experts,capacity", [
     (1, 1, 1, 0), (1, 2, 8, 0), (3, 1, 2, 1), (20, 2, 8, 0), (31, 1, 5, 4), (33, 3, 7, 9), (512, 1, 3, 0), (511, 2, 64, 20), (1111, 3, 61, 0),
-    (2000, 8, 256, 70), (4097, 1, 1, 5000), (5000, 4, 2048, 12), (777, 5, 513, 0), (16384, 2, 64, 640), (40000, 8, 1000, 0), (9000, 7, 2, 31000)])
+    (2000, 8, 256, 70), (4097, 1, 1, 5000), (5000, 4, 2048, 12), (777, 5, 513, 0), (16384, 2, 64, 640), (40000, 8, 1000, 0), (9000, 7, 2, 31000),
+    (16385, 2, 64, 0), (33000, 1, 3, 12000), (50001, 3, 2048, 70), (100000, 2, 7, 0)])
 def test_sort(tokens, k, experts, capacity):
     for seed, bad in ((1, 0.0), (2, 0.3)):
         ids = choose(tokens, k, experts, seed, bad)

@@ -26,12 +26,16 @@ def test_rows():
 
 def test_sort_refuses(L):
     def call(**kw):
-        a = dict(ids=P, tokens=10, k=2, experts=4, capacity=0, slots=P, sources=P, counts=P, offsets=P, stream=0) | kw
+        a = dict(ids=P, tokens=10, k=2, experts=4, capacity=0, slots=P, sources=P, counts=P, offsets=P, ws=0, wsb=0, stream=0) | kw
         return L.pf_expert_sort(*a.values())
     for name in ("ids", "slots", "sources", "counts", "offsets"):
         assert call(**{name: 0}) == INVALID and call(**{name: P + 2}) == INVALID
     assert call(tokens=-1) == INVALID and call(k=0) == INVALID and call(experts=0) == INVALID and call(capacity=-1) == INVALID
     assert call(experts=2049) == UNSUPPORTED and call(tokens=1 << 30) == UNSUPPORTED and call(capacity=1 << 29) == UNSUPPORTED
+    need = pf.pf_expert_sort_workspace(100000, 2, 64)
+    assert need > 0 and need % 256 == 0 and pf.pf_expert_sort_workspace(100, 2, 64) == 0 and pf.pf_expert_sort_workspace(100000, 2, 4000) == 0
+    for ws, room in ((0, need), (P + 16, need), (P, need - 1)):
+        assert call(tokens=100000, experts=64, ws=ws, wsb=room) == WORKSPACE
 
 
 def test_rows_are_refused(L):
