@@ -11,6 +11,7 @@
 // integer product in parts of a turn, sine and cosine in fp32) are computed once for all of them and stay in registers.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "pf_f32x2.cuh"
 #include "pf_internal.h"
@@ -169,6 +170,91 @@ struct RopeWalk {
     }
 };
 
+// A warp's cosines (and sines): those of a token's pairs, then from a multiple of four on those of eight pairs that are not turned.
+__host__ __device__ constexpr int rope_still(int half) { return (half + 3) / 4 * 4; }
+__host__ __device__ constexpr int rope_angles(int half) { return rope_still(half) + 8; }
+
+// Which elements of a row a lane has: na from ia on and nb from ib on (kN each, fewer in the last pieces of rows of odd widths), and its pairs.
+struct RopeShare {
+    int ia, ib, na, nb, pair_a, pair_b;      // pair_b: PF_ROPE_PAIRS only
+};
+template <int kN, bool kPairs, bool kMasked>
+__device__ __forceinline__ RopeShare rope_share(int l, int dim, int rot) {
+    const int half = rot / 2;
+    RopeShare s;
+    if constexpr (!kMasked) {
+        // pieces of each half of what is turned, then of each half of what is not
+        const bool turned = kN * l < half;
+        s.ia = turned ? kN * l : rot + kN * l - half;
+        s.ib = s.ia + (turned ? half : (dim - rot) / 2);
+        s.na = s.nb = 2 * kN * l < dim ? kN : 0;
+        s.pair_a = turned ? (kPairs ? s.ia / 2 : s.ia) : rope_still(half);
+        s.pair_b = turned ? s.ib / 2 : rope_still(half);
+    } else {
+        // as many lanes as what is turned takes; two pieces side by side where pairs are neighbours, and of what is not turned
+        const int lanes = kPairs ? (rot + 2 * kN - 1) / (2 * kN) : (half + kN - 1) / kN;
+        const bool turned = l < lanes, apart = turned && !kPairs;
+        const int end = apart ? half : turned ? rot : dim;
+        s.ia = apart ? kN * l : turned ? 2 * kN * l : rot + 2 * kN * (l - lanes);
+        s.na = max(0, min(kN, end - s.ia));
+        s.ib = s.ia + (apart ? half : kN);
+        s.nb = apart ? s.na : max(0, min(kN, end - s.ib));
+        s.pair_a = turned ? kN * l : rope_still(half);
+        s.pair_b = turned ? kN * l + kN / 2 : rope_still(half);
+    }
+    return s;
+}
+// Eight elements of a row of any alignment, of which n exist.  bf16: put together from the aligned words that hold them.
+__device__ __forceinline__ void load_some(const float* p, int n, F2 (&x)[4]) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = f2(v[2 * i], v[2 * i + 1]);
+}
+__device__ __forceinline__ void load_some(const __nv_bfloat16* p, int n, F2 (&x)[4]) {
+    const unsigned odd = static_cast<unsigned>(reinterpret_cast<uintptr_t>(p) >> 1) & 1u;
+    const unsigned* const low = reinterpret_cast<const unsigned*>(p - odd);
+    unsigned w[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = n > 0 && 2 * i - static_cast<int>(odd) < n ? low[i] : 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned t = __funnelshift_r(w[i], w[i + 1], odd * 16);
+        x[i] = f2(2 * i < n ? __uint_as_float(t << 16) : 0.f, 2 * i + 1 < n ? __uint_as_float(t & 0xffff0000u) : 0.f);
+    }
+}
+__device__ __forceinline__ void store_some(float* p, int n, const F2 (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 v = split(x[i]);
+        if (2 * i < n) p[2 * i] = v.x;
+        if (2 * i + 1 < n) p[2 * i + 1] = v.y;
+    }
+}
+__device__ __forceinline__ void store_some(__nv_bfloat16* p, int n, const F2 (&x)[4]) {
+    __nv_bfloat162 t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 v = split(x[i]);
+        t[i] = __floats2bfloat162_rn(v.x, v.y);
+    }
+    if ((reinterpret_cast<uintptr_t>(p) & 2) == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (2 * i + 1 < n) *reinterpret_cast<__nv_bfloat162*>(p + 2 * i) = t[i];
+            else if (2 * i < n) p[2 * i] = t[i].x;
+        }
+    } else {
+        if (n > 0) p[0] = t[0].x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i < 3 && 2 * i + 2 < n) *reinterpret_cast<__nv_bfloat162*>(p + 2 * i + 1) = __nv_bfloat162(t[i].y, t[i < 3 ? i + 1 : 3].x);
+            else if (2 * i + 1 < n) p[2 * i + 1] = t[i].y;
+        }
+    }
+}
+
 // kLanes lanes to a row (the power of two from the row's pieces / 2 on), 32 / kLanes rows of a warp at a time.  Each lane keeps the
 // pieces of its next kStages - 1 rows on the way into its own places of shared memory, across units: what a warp waits for was asked for rows
 // ago, and nothing is exchanged between lanes but the sums and the angles.  Few rows ahead are enough, and more cost time (16384 x 40 heads of 128: forward
@@ -176,29 +262,28 @@ struct RopeWalk {
 template <bool kBwd> constexpr int kRopeStages = kBwd ? 2 : 3;
 template <bool kBwd> constexpr int kRopePieces = kBwd ? 4 : 2;      // 16-byte pieces of a lane for a row: two of x, two of the gradient
 template <bool kBwd> constexpr int kRopeRing = kRopeWarps * kRopeStages<kBwd> * kRopePieces<kBwd> * 32 * 16;
-// Behind them, for each warp, the cosines of a token's pairs and those of what is not turned, then the sines.
-constexpr int kStill = 8;
-__host__ __device__ constexpr int rope_angles(int half) { return half + kStill; }
+// (kMasked: no places, but room for the sums of dw.)
+template <bool kBwd, bool kMasked> constexpr int kRopeBefore = !kMasked ? kRopeRing<kBwd> : kBwd ? 16384 : 0;
+// Behind them each warp's cosines, then its sines.
 
-template <typename T, int kLanes, bool kPairs, bool kBwd>
+// kMasked: rows of any width and alignment, element loads straight to registers.
+template <typename T, int kLanes, bool kPairs, bool kBwd, bool kMasked>
 __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams p) {
-    constexpr int kN = Piece<T>::kN, kRows = 32 / kLanes, kStages = kRopeStages<kBwd>, kPieces = kRopePieces<kBwd>, kStage = kPieces * 32 * 16;
+    constexpr int kN = kMasked ? 8 : Piece<T>::kN, kRows = 32 / kLanes, kStages = kRopeStages<kBwd>, kPieces = kRopePieces<kBwd>, kStage = kPieces * 32 * 16;
     constexpr bool kExact = sizeof(T) == 4;
-    static_assert(kStill >= kN, "");
     extern __shared__ __align__(16) unsigned char rope_smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bool key = static_cast<int>(blockIdx.x) >= p.side[0].blocks;
     const RopeSide& s = p.side[key ? 1 : 0];
     const int block = static_cast<int>(blockIdx.x) - (key ? p.side[0].blocks : 0);
-    // this lane's pieces: the first ones of a row cover the pairs, the others what is not turned
     const int l = lane % kLanes, row = lane / kLanes, half = p.rot / 2, tokens = static_cast<int>(p.tokens);
-    const bool there = 2 * kN * l < p.dim, turned = kN * l < half;
-    const int ia = turned ? kN * l : p.rot + kN * l - half, ib = ia + (turned ? half : (p.dim - p.rot) / 2);
+    const RopeShare share = rope_share<kN, kPairs, kMasked>(l, p.dim, p.rot);
+    const int ia = share.ia, ib = share.ib, pair_a = share.pair_a, pair_b = share.pair_b;
+    const bool there = share.na > 0;
     unsigned char* const ring = rope_smem + (warp * kStages * kPieces * 32 + lane) * 16;
     const uint32_t ring_at = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
-    float* const cosines = reinterpret_cast<float*>(rope_smem + kRopeRing<kBwd>) + warp * 2 * rope_angles(half);
+    float* const cosines = reinterpret_cast<float*>(rope_smem + kRopeBefore<kBwd, kMasked>) + warp * 2 * rope_angles(half);
     float* const sines = cosines + rope_angles(half);
-    const int pair_a = turned ? (kPairs ? ia / 2 : ia) : half, pair_b = turned ? ib / 2 : half;      // pair_b: PF_ROPE_PAIRS only
     RopeWalk ahead, at;      // rows to ask for, rows to compute
     {
         const unsigned unit = static_cast<unsigned>(block) * kRopeWarps + warp, per = static_cast<unsigned>(s.units_per_token);
@@ -214,6 +299,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     auto ask = [&](int stage) {
+        if constexpr (kMasked) return;
         if (ahead.token < tokens) {
             if (there && ahead.h + row < ahead.end) {
                 const uint32_t to = ring_at + stage * kStage;
@@ -240,12 +326,12 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
     for (int i = 0; i < kStages - 1; ++i) ask(i);
     auto position_of = [&](const RopeWalk& w) -> int64_t { return w.token >= tokens ? 0 : p.positions ? p.positions[w.token] : w.token; };
     int64_t position = position_of(at);
-    // the turns of this lane's first angles for a position (those of rows of more than 128 pairs are made again for each token)
+    // the turns of this lane's first angles for a position (those of rows of more than 64 pairs are made again for each token)
     constexpr int kKept = 2;
     uint64_t each[kKept];
 #pragma unroll
     for (int i = 0; i < kKept; ++i) each[i] = lane + 32 * i < half ? turn_per_position(p.inv_freq[lane + 32 * i]) : 0;
-    if (lane < kStill) {
+    if (lane < rope_angles(half) - half) {
         cosines[half + lane] = 1.f;
         sines[half + lane] = 0.f;
     }
@@ -253,11 +339,16 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
 #pragma unroll
     for (int i = 0; i < kN / 2; ++i) wa[i] = wb[i] = f2(1.f, 1.f);
     if (s.w && there) {
-        Piece<T> t;
-        t.load(static_cast<const T*>(s.w) + ia);
-        t.get(wa);
-        t.load(static_cast<const T*>(s.w) + ib);
-        t.get(wb);
+        if constexpr (kMasked) {
+            load_some(static_cast<const T*>(s.w) + ia, share.na, wa);
+            load_some(static_cast<const T*>(s.w) + ib, share.nb, wb);
+        } else {
+            Piece<T> t;
+            t.load(static_cast<const T*>(s.w) + ia);
+            t.get(wa);
+            t.load(static_cast<const T*>(s.w) + ib);
+            t.get(wb);
+        }
     }
     F2 dwa[kN / 2], dwb[kN / 2];
 #pragma unroll
@@ -288,22 +379,36 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
         position = position_of(next);
         T* out = static_cast<T*>(s.out) + at.token * s.ldo + (at.h + row) * s.so;
         for (; at.h < at.end; at.h += kRows, out += kRows * s.so) {
-            __syncwarp();
-            ask(stage == 0 ? kStages - 1 : stage - 1);      // the place that the row before has left
-            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-            const unsigned char* const in = ring + stage * kStage;
-            stage = stage == kStages - 1 ? 0 : stage + 1;
             const bool live = at.h + row < at.end, on = there && live;
-            F2 a[kN / 2], b[kN / 2];
-            Piece<T> xa, xb;
-            xa.raw = {};
-            xb.raw = {};
-            if (on) {
-                xa.load(in);
-                xb.load(in + 512);
+            F2 a[kN / 2], b[kN / 2], ea[kN / 2], eb[kN / 2];      // x, and the upstream gradient
+            if constexpr (kMasked) {
+                const T* const x = x0 + at.token * s.ldx + at.h * s.sx;
+                load_some(x + ia, on ? share.na : 0, a);
+                load_some(x + ib, on ? share.nb : 0, b);
+                if constexpr (kBwd) {
+                    const T* const g = g0 + at.token * s.ldg + at.h * s.sg;
+                    load_some(g + ia, on ? share.na : 0, ea);
+                    load_some(g + ib, on ? share.nb : 0, eb);
+                }
+            } else {
+                __syncwarp();
+                ask(stage == 0 ? kStages - 1 : stage - 1);      // the place that the row before has left
+                asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+                const unsigned char* const in = ring + stage * kStage;
+                stage = stage == kStages - 1 ? 0 : stage + 1;
+                auto get = [&](F2 (&x)[kN / 2], int piece) {
+                    Piece<T> t;
+                    t.raw = {};
+                    if (on) t.load(in + 512 * piece);
+                    t.get(x);
+                };
+                get(a, 0);
+                get(b, 1);
+                if constexpr (kBwd) {
+                    get(ea, 2);
+                    get(eb, 3);
+                }
             }
-            xa.get(a);
-            xb.get(b);
             F2 sq2 = mul2(a[0], a[0]);
 #pragma unroll
             for (int i = 1; i < kN / 2; ++i) sq2 = fma2(a[i], a[i], sq2);
@@ -319,15 +424,6 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
                 for (int i = 0; i < kN / 2; ++i) { a[i] = mul2(a[i], mul2(rr, wa[i])); b[i] = mul2(b[i], mul2(rr, wb[i])); }
                 turn<kN, kPairs, false>(a, b, c, sn);
             } else {
-                F2 ea[kN / 2], eb[kN / 2];
-                xa.raw = {};
-                xb.raw = {};
-                if (on) {
-                    xa.load(in + 1024);
-                    xb.load(in + 1536);
-                }
-                xa.get(ea);
-                xb.get(eb);
                 turn<kN, kPairs, true>(ea, eb, c, sn);
                 F2 dot2 = f2(0.f, 0.f);
 #pragma unroll
@@ -346,7 +442,10 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
 #pragma unroll
                 for (int i = 0; i < kN / 2; ++i) { a[i] = mul2(rr, fma2(a[i], dd, ea[i])); b[i] = mul2(rr, fma2(b[i], dd, eb[i])); }
             }
-            if (on) {
+            if constexpr (kMasked) {
+                store_some(out + ia, on ? share.na : 0, a);
+                store_some(out + ib, on ? share.nb : 0, b);
+            } else if (on) {
                 Piece<T>::store(out + ia, a);
                 Piece<T>::store(out + ib, b);
             }
@@ -358,7 +457,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
         if (!s.partial) return;
         // rows of a warp, then warps in order
         float* const red = reinterpret_cast<float*>(rope_smem);      // (16 KB of the pieces' places at most)
-        static_assert(kRopeWarps * 2 * kN * kLanes * 4 <= kRopeRing<kBwd>, "");
+        static_assert(kRopeWarps * 2 * kN * kLanes * 4 <= kRopeBefore<kBwd, kMasked>, "");
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
@@ -375,18 +474,17 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
         }
         __syncthreads();
         for (int i = threadIdx.x; i < 2 * kN * kLanes; i += kRopeThreads) {
-            const int cl = i % kLanes, e = i / kLanes;
-            if (2 * kN * cl >= p.dim) continue;
+            const int e = i / kLanes;
+            const RopeShare q = rope_share<kN, kPairs, kMasked>(i % kLanes, p.dim, p.rot);
+            if (e < kN ? e >= q.na : e - kN >= q.nb) continue;
             float sum = 0.f;
-            for (int w = 0; w < kRopeWarps; ++w) sum += red[(w * 2 * kN + e) * kLanes + cl];
-            const bool t = kN * cl < half;
-            const int a0 = t ? kN * cl : p.rot + kN * cl - half, b0 = a0 + (t ? half : (p.dim - p.rot) / 2);
-            s.partial[static_cast<int64_t>(block) * p.dim + (e < kN ? a0 + e : b0 + e - kN)] = sum;
+            for (int w = 0; w < kRopeWarps; ++w) sum += red[(w * 2 * kN + e) * kLanes + i % kLanes];
+            s.partial[static_cast<int64_t>(block) * p.dim + (e < kN ? q.ia + e : q.ib + e - kN)] = sum;
         }
     }
 }
 
-// Rows of any width, pitch and alignment: a warp to a row, element after element, the other element of a pair read again.
+// Rows that are too wide for a warp's registers: a warp to a row, element after element, the other element of a pair read again.
 template <typename T, bool kPairs, bool kBwd>
 __global__ void __launch_bounds__(kAnyThreads) rope_any_kernel(const RopeParams p) {
     extern __shared__ float any_smem[];      // per warp: angles of a token, then (backward) sums for dw
@@ -507,7 +605,7 @@ bool rows_in_pieces(const RowsView& v, int dtype) {
 
 // How the rows of a call are divided: both kernels walk units of (token, some of its heads).
 struct RopePlan {
-    bool pieces;
+    enum Kind { kAny, kMasked, kPieces } kind;
     int lanes, warps;            // lanes of a row, warps of a block
     int blocks[2], heads_per_unit[2], units_per_token[2];
     RopeSide side(int i, RopeSide s) const {
@@ -524,16 +622,24 @@ struct RopePlan {
 // Blocks of an SM: two of the vector kernels, whose registers (80 for three forward ones) would otherwise spill: 16384 x 40 heads of 128 forward 66 us with
 // three, 59.5 with two.  Twice as many of the others.
 constexpr int kRopeBlocksPerSm = 2;
-RopePlan rope_plan(int64_t tokens, const int (&heads)[2], int dim, int rot, int dtype, bool pieces) {
+RopePlan rope_plan(int64_t tokens, const int (&heads)[2], int dim, int rot, bool pairs, int dtype, bool pieces) {
     RopePlan pl = {};
     const int n = 16 / static_cast<int>(dtype_size(dtype));
-    pl.pieces = pieces && dim % (2 * n) == 0 && rot % (2 * n) == 0 && dim / (2 * n) <= 32 && rot / 2 <= kMaxPairs;
-    pl.lanes = 32;
-    if (pl.pieces)
-        for (pl.lanes = 2; pl.lanes < dim / (2 * n);) pl.lanes *= 2;
-    pl.warps = pl.pieces ? kRopeWarps : kAnyWarps;
-    const int rows = pl.pieces ? 32 / pl.lanes : 1;
-    const int64_t most = static_cast<int64_t>(num_sms()) * kRopeBlocksPerSm * (pl.pieces ? 1 : 2);
+    const int half = rot / 2;
+    if (pieces && dim % (2 * n) == 0 && rot % (2 * n) == 0 && dim / (2 * n) <= 32 && half <= kMaxPairs) {
+        pl.kind = RopePlan::kPieces;
+        pl.lanes = dim / (2 * n);
+    } else {
+        pl.lanes = static_cast<int>((pairs ? ceil_div(rot, 16) : ceil_div(half, 8)) + ceil_div(dim - rot, 16));
+        pl.kind = pl.lanes <= 32 && half <= kMaxPairs ? RopePlan::kMasked : RopePlan::kAny;
+    }
+    const bool any = pl.kind == RopePlan::kAny;
+    int lanes = 2;
+    while (lanes < pl.lanes && lanes < 32) lanes *= 2;
+    pl.lanes = lanes;
+    pl.warps = any ? kAnyWarps : kRopeWarps;
+    const int rows = any ? 1 : 32 / pl.lanes;
+    const int64_t most = static_cast<int64_t>(num_sms()) * kRopeBlocksPerSm * (any ? 2 : 1);
     // Blocks by the time that a side takes: a warp's turn at some heads, and what a unit costs besides, kUnit of one.
     constexpr double kUnit = 0.5;
     int64_t turns[2] = {ceil_div(heads[0], rows), ceil_div(heads[1], rows)};      // of a token
@@ -556,33 +662,37 @@ RopePlan rope_plan(int64_t tokens, const int (&heads)[2], int dim, int rot, int 
     return pl;
 }
 
-template <typename T, int kLanes, bool kPairs, bool kBwd>
+template <typename T, int kLanes, bool kPairs, bool kBwd, bool kMasked>
 cudaError_t rope_styled(const RopeParams& p, int blocks, cudaStream_t stream) {
     static std::atomic<uint64_t> allowed{0};
-    const auto kernel = rope_kernel<T, kLanes, kPairs, kBwd>;
-    const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), kRopeRing<kBwd> + kRopeWarps * rope_angles(kMaxPairs) * sizeof(float2), allowed);
+    constexpr int kBefore = kRopeBefore<kBwd, kMasked>, kAngle = kRopeWarps * 2 * static_cast<int>(sizeof(float));
+    const auto kernel = rope_kernel<T, kLanes, kPairs, kBwd, kMasked>;
+    const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), kBefore + kAngle * rope_angles(kMaxPairs), allowed);
     if (e != cudaSuccess) return e;
-    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kRopeThreads, kRopeRing<kBwd> + kRopeWarps * rope_angles(p.rot / 2) * sizeof(float2), 1, stream, p);
+    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kRopeThreads, kBefore + kAngle * rope_angles(p.rot / 2), 1, stream, p);
 }
-template <typename T, int kLanes, bool kBwd>
-cudaError_t rope_pieces(const RopeParams& p, bool pairs, int blocks, cudaStream_t stream) {
-    return pairs ? rope_styled<T, kLanes, true, kBwd>(p, blocks, stream) : rope_styled<T, kLanes, false, kBwd>(p, blocks, stream);
+template <typename T, bool kBwd, bool kMasked>
+cudaError_t rope_by_lanes(const RopeParams& p, int lanes, bool pairs, int blocks, cudaStream_t stream) {
+    const auto run = [&](auto n) {
+        constexpr int kLanes = decltype(n)::value;
+        return pairs ? rope_styled<T, kLanes, true, kBwd, kMasked>(p, blocks, stream) : rope_styled<T, kLanes, false, kBwd, kMasked>(p, blocks, stream);
+    };
+    switch (lanes) {
+        case 2: return run(std::integral_constant<int, 2>());
+        case 4: return run(std::integral_constant<int, 4>());
+        case 8: return run(std::integral_constant<int, 8>());
+        case 16: return run(std::integral_constant<int, 16>());
+        default: return run(std::integral_constant<int, 32>());
+    }
 }
 template <typename T, bool kBwd>
 cudaError_t rope_launch(const RopeParams& p, const RopePlan& pl, bool pairs, cudaStream_t stream) {
     const int blocks = pl.blocks[0] + pl.blocks[1];
-    if (!pl.pieces) {
-        const size_t smem = sizeof(float) * kAnyWarps * (p.rot + (kBwd ? p.dim : 0));      // at most 32 KB
-        const auto kernel = pairs ? rope_any_kernel<T, true, kBwd> : rope_any_kernel<T, false, kBwd>;
-        return launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kAnyThreads, smem, 1, stream, p);
-    }
-    switch (pl.lanes) {
-        case 2: return rope_pieces<T, 2, kBwd>(p, pairs, blocks, stream);
-        case 4: return rope_pieces<T, 4, kBwd>(p, pairs, blocks, stream);
-        case 8: return rope_pieces<T, 8, kBwd>(p, pairs, blocks, stream);
-        case 16: return rope_pieces<T, 16, kBwd>(p, pairs, blocks, stream);
-        default: return rope_pieces<T, 32, kBwd>(p, pairs, blocks, stream);
-    }
+    if (pl.kind == RopePlan::kPieces) return rope_by_lanes<T, kBwd, false>(p, pl.lanes, pairs, blocks, stream);
+    if (pl.kind == RopePlan::kMasked) return rope_by_lanes<T, kBwd, true>(p, pl.lanes, pairs, blocks, stream);
+    const size_t smem = sizeof(float) * kAnyWarps * (p.rot + (kBwd ? p.dim : 0));      // at most 32 KB
+    const auto kernel = pairs ? rope_any_kernel<T, true, kBwd> : rope_any_kernel<T, false, kBwd>;
+    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kAnyThreads, smem, 1, stream, p);
 }
 
 int validate_rope(const RowsView (&x)[2], const void* const (&w)[2], const int64_t* positions, const float* inv_freq, const RowsView (&out)[2],
@@ -620,7 +730,7 @@ int pf_qk_norm_rope_fwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
     for (int i = 0; i < 2; ++i)
         if (heads[i] > 0)
             pieces = pieces && rows_in_pieces(x[i], dtype) && rows_in_pieces(out[i], dtype) && reinterpret_cast<uintptr_t>(w[i]) % 16 == 0;
-    const RopePlan pl = rope_plan(tokens, heads, dim, rot_dim, dtype, pieces);
+    const RopePlan pl = rope_plan(tokens, heads, dim, rot_dim, style == PF_ROPE_PAIRS, dtype, pieces);
     RopeParams p = {};
     p.positions = positions;
     p.inv_freq = inv_freq;
@@ -672,7 +782,7 @@ int pf_qk_norm_rope_bwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
             if (dw[i] && !(flags & PF_GRAD_ACCUMULATE)) PF_CUDA(cudaMemsetAsync(dw[i], 0, dim * dtype_size(wtype), stream));
         return PF_OK;
     }
-    const RopePlan pl = rope_plan(tokens, heads, dim, rot_dim, dtype, pieces);
+    const RopePlan pl = rope_plan(tokens, heads, dim, rot_dim, style == PF_ROPE_PAIRS, dtype, pieces);
     RopeParams p = {};
     p.positions = positions;
     p.inv_freq = inv_freq;
