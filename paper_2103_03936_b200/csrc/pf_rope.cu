@@ -34,6 +34,7 @@ struct RopeSide {
     int64_t ldx, sx, ldg, sg, ldo, so;
     int heads, heads_per_unit, units_per_token, blocks;
     int step_tokens, step_parts;      // from a warp's unit to its next
+    bool across;                      // the rows of a warp are one head's of several tokens (a unit is as many tokens), not several heads' of one
 };
 struct RopeParams {
     RopeSide side[2];
@@ -266,8 +267,9 @@ template <bool kBwd> constexpr int kRopeRing = kRopeWarps * kRopeStages<kBwd> * 
 template <bool kBwd, bool kMasked> constexpr int kRopeBefore = !kMasked ? kRopeRing<kBwd> : kBwd ? 16384 : 0;
 // Behind them each warp's cosines, then its sines.
 
-// kMasked: rows of any width and alignment, element loads straight to registers.
-template <typename T, int kLanes, bool kPairs, bool kBwd, bool kMasked>
+// kMasked: rows of any width and alignment, element loads straight to registers.  kAcross: kernels that know sides with RopeSide::across (apart, for the
+// registers that they need: 16384 x 40 heads of 128 backward 79 -> 89 us).
+template <typename T, int kLanes, bool kPairs, bool kBwd, bool kMasked, bool kAcross>
 __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams p) {
     constexpr int kN = kMasked ? 8 : Piece<T>::kN, kRows = 32 / kLanes, kStages = kRopeStages<kBwd>, kPieces = kRopePieces<kBwd>, kStage = kPieces * 32 * 16;
     constexpr bool kExact = sizeof(T) == 4;
@@ -275,6 +277,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bool key = static_cast<int>(blockIdx.x) >= p.side[0].blocks;
     const RopeSide& s = p.side[key ? 1 : 0];
+    const bool across = kAcross && s.across;
     const int block = static_cast<int>(blockIdx.x) - (key ? p.side[0].blocks : 0);
     const int l = lane % kLanes, row = lane / kLanes, half = p.rot / 2, tokens = static_cast<int>(p.tokens);
     const RopeShare share = rope_share<kN, kPairs, kMasked>(l, p.dim, p.rot);
@@ -289,11 +292,14 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
         const unsigned unit = static_cast<unsigned>(block) * kRopeWarps + warp, per = static_cast<unsigned>(s.units_per_token);
         ahead.token = static_cast<int>(unit / per);
         ahead.part = static_cast<int>(unit - ahead.token * per);
+        if (across) ahead.token *= kRows;
         ahead.enter(s);
         at = ahead;
     }
-    const T* const x0 = static_cast<const T*>(s.x) + row * s.sx;
-    const T* const g0 = static_cast<const T*>(s.g) + row * s.sg;
+    const int turn_heads = across ? 1 : kRows;      // from a warp's rows to its next
+    const T* const x0 = static_cast<const T*>(s.x) + row * (across ? s.ldx : s.sx);
+    const T* const g0 = static_cast<const T*>(s.g) + row * (across ? s.ldg : s.sg);
+    auto has_row = [&](const RopeWalk& w) { return across ? w.token + row < tokens : w.h + row < w.end; };
     const T* xp = x0 + ahead.token * s.ldx + ahead.h * s.sx;
     const T* gp = g0 + ahead.token * s.ldg + ahead.h * s.sg;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -301,7 +307,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
     auto ask = [&](int stage) {
         if constexpr (kMasked) return;
         if (ahead.token < tokens) {
-            if (there && ahead.h + row < ahead.end) {
+            if (there && has_row(ahead)) {
                 const uint32_t to = ring_at + stage * kStage;
                 fetch16(to, xp + ia);
                 fetch16(to + 512, xp + ib);
@@ -310,28 +316,36 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
                     fetch16(to + 1536, gp + ib);
                 }
             }
-            ahead.h += kRows;
+            ahead.h += turn_heads;
             if (ahead.h >= ahead.end) {
                 ahead.next_unit(s);
                 xp = x0 + ahead.token * s.ldx + ahead.h * s.sx;
                 if constexpr (kBwd) gp = g0 + ahead.token * s.ldg + ahead.h * s.sg;
             } else {
-                xp += kRows * s.sx;
-                if constexpr (kBwd) gp += kRows * s.sg;
+                xp += turn_heads * s.sx;
+                if constexpr (kBwd) gp += turn_heads * s.sg;
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i) ask(i);
-    auto position_of = [&](const RopeWalk& w) -> int64_t { return w.token >= tokens ? 0 : p.positions ? p.positions[w.token] : w.token; };
+    auto position_of = [&](const RopeWalk& w) -> int64_t {      // (across: of this lane's token)
+        const int token = across ? w.token + row : w.token;
+        return token >= tokens ? 0 : p.positions ? p.positions[token] : token;
+    };
     int64_t position = position_of(at);
     // the turns of this lane's first angles for a position (those of rows of more than 64 pairs are made again for each token)
     constexpr int kKept = 2;
     uint64_t each[kKept];
 #pragma unroll
     for (int i = 0; i < kKept; ++i) each[i] = lane + 32 * i < half ? turn_per_position(p.inv_freq[lane + 32 * i]) : 0;
-    if (lane < rope_angles(half) - half) {
+    // (across: those of all pairs for the block)
+    uint64_t* const turns = reinterpret_cast<uint64_t*>(rope_smem + kRopeBefore<kBwd, kMasked>);
+    if (across) {
+        for (int i = threadIdx.x; i < half; i += kRopeThreads) turns[i] = turn_per_position(p.inv_freq[i]);
+        __syncthreads();
+    } else if (lane < rope_angles(half) - half) {
         cosines[half + lane] = 1.f;
         sines[half + lane] = 0.f;
     }
@@ -356,30 +370,41 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
     const float inv_dim = 1.f / static_cast<float>(p.dim);
     int stage = 0;
     while (at.token < tokens) {
-        __syncwarp();
-        auto angle = [&](int i, uint64_t turns) {
-            const float2 v = turn_of<kExact>(position, turns);
-            cosines[i] = v.x;
-            sines[i] = v.y;
-        };
-#pragma unroll
-        for (int i = 0; i < kKept; ++i)
-            if (lane + 32 * i < half) angle(lane + 32 * i, each[i]);
-        for (int i = lane + 32 * kKept; i < half; i += 32) angle(i, turn_per_position(p.inv_freq[i]));
-        __syncwarp();
         F2 c[kN / 2], sn[kN / 2];
+        if (across) {      // each lane the angles of its own pairs
 #pragma unroll
-        for (int i = 0; i < kN / 2; ++i) {
-            const int at_pair = !kPairs ? pair_a + 2 * i : i < kN / 4 ? pair_a + 2 * i : pair_b + 2 * i - kN / 2;
-            c[i] = *reinterpret_cast<const F2*>(cosines + at_pair);
-            sn[i] = *reinterpret_cast<const F2*>(sines + at_pair);
+            for (int i = 0; i < kN; ++i) {
+                const int pair = !kPairs || i < kN / 2 ? pair_a + i : pair_b + i - kN / 2;
+                const float2 v = pair < half ? turn_of<kExact>(position, turns[pair]) : make_float2(1.f, 0.f);
+                const float2 cv = split(c[i / 2]), sv = split(sn[i / 2]);
+                c[i / 2] = i % 2 ? f2(cv.x, v.x) : f2(v.x, 0.f);
+                sn[i / 2] = i % 2 ? f2(sv.x, v.y) : f2(v.y, 0.f);
+            }
+        } else {
+            __syncwarp();
+            auto angle = [&](int i, uint64_t turn_each) {
+                const float2 v = turn_of<kExact>(position, turn_each);
+                cosines[i] = v.x;
+                sines[i] = v.y;
+            };
+#pragma unroll
+            for (int i = 0; i < kKept; ++i)
+                if (lane + 32 * i < half) angle(lane + 32 * i, each[i]);
+            for (int i = lane + 32 * kKept; i < half; i += 32) angle(i, turn_per_position(p.inv_freq[i]));
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < kN / 2; ++i) {
+                const int at_pair = !kPairs ? pair_a + 2 * i : i < kN / 4 ? pair_a + 2 * i : pair_b + 2 * i - kN / 2;
+                c[i] = *reinterpret_cast<const F2*>(cosines + at_pair);
+                sn[i] = *reinterpret_cast<const F2*>(sines + at_pair);
+            }
         }
         RopeWalk next = at;
         next.next_unit(s);
         position = position_of(next);
-        T* out = static_cast<T*>(s.out) + at.token * s.ldo + (at.h + row) * s.so;
-        for (; at.h < at.end; at.h += kRows, out += kRows * s.so) {
-            const bool live = at.h + row < at.end, on = there && live;
+        T* out = static_cast<T*>(s.out) + at.token * s.ldo + at.h * s.so + row * (across ? s.ldo : s.so);
+        for (; at.h < at.end; at.h += turn_heads, out += turn_heads * s.so) {
+            const bool live = has_row(at), on = there && live;
             F2 a[kN / 2], b[kN / 2], ea[kN / 2], eb[kN / 2];      // x, and the upstream gradient
             if constexpr (kMasked) {
                 const T* const x = x0 + at.token * s.ldx + at.h * s.sx;
@@ -607,14 +632,15 @@ bool rows_in_pieces(const RowsView& v, int dtype) {
 struct RopePlan {
     enum Kind { kAny, kMasked, kPieces } kind;
     int lanes, warps;            // lanes of a row, warps of a block
-    int blocks[2], heads_per_unit[2], units_per_token[2];
+    int blocks[2], heads_per_unit[2], units_per_token[2], tokens_per_unit[2];
     RopeSide side(int i, RopeSide s) const {
         s.heads_per_unit = heads_per_unit[i];
         s.units_per_token = units_per_token[i];
         s.blocks = blocks[i];
         if (s.heads > 0) {
-            s.step_tokens = blocks[i] * warps / units_per_token[i];
+            s.step_tokens = blocks[i] * warps / units_per_token[i] * tokens_per_unit[i];
             s.step_parts = blocks[i] * warps % units_per_token[i];
+            s.across = tokens_per_unit[i] > 1;
         }
         return s;
     }
@@ -640,42 +666,50 @@ RopePlan rope_plan(int64_t tokens, const int (&heads)[2], int dim, int rot, bool
     pl.warps = any ? kAnyWarps : kRopeWarps;
     const int rows = any ? 1 : 32 / pl.lanes;
     const int64_t most = static_cast<int64_t>(num_sms()) * kRopeBlocksPerSm * (any ? 2 : 1);
-    // Blocks by the time that a side takes: a warp's turn at some heads, and what a unit costs besides, kUnit of one.
-    constexpr double kUnit = 0.5;
-    int64_t turns[2] = {ceil_div(heads[0], rows), ceil_div(heads[1], rows)};      // of a token
-    const double q = turns[0] ? turns[0] + kUnit : 0, k = turns[1] ? turns[1] + kUnit : 0;
+    // A side of few heads fills a warp with one head's rows of several tokens, each with angles of its own (8192 tokens of one head of 64: 8.3 us
+    // with idle lanes, 4.0 so).
+    double time[2];      // of a side by one warp, in turns of a warp at its rows; what a unit costs besides is kUnit of one (kOwn with own angles)
+    constexpr double kUnit = 0.5, kOwn = 1.0;
+    for (int i = 0; i < 2; ++i) {
+        const bool across = pl.kind == RopePlan::kPieces && pl.lanes < 32 && heads[i] > 0 && heads[i] * 2 <= rows && tokens > 1;
+        pl.tokens_per_unit[i] = across ? rows : 1;
+        time[i] = heads[i] == 0 ? 0.0 : across ? (heads[i] + kOwn) / rows : ceil_div(heads[i], rows) + kUnit;
+    }
     for (int i = 0; i < 2; ++i) {
         if (heads[i] == 0) continue;
-        const int64_t share = std::max<int64_t>(1, static_cast<int64_t>(most * (i ? k : q) / (q + k)));
+        const int64_t share = std::max<int64_t>(1, static_cast<int64_t>(most * time[i] / (time[0] + time[1])));
+        const int64_t turns = ceil_div(heads[i], rows);
+        pl.heads_per_unit[i] = heads[i];
         // units as large as leave the warps equal shares
         double best = 0;
-        for (int64_t units = 1; units <= turns[i]; units *= 2) {
-            const int64_t each = ceil_div(turns[i], units);
-            const double time = static_cast<double>(ceil_div(tokens * ceil_div(turns[i], each), share * pl.warps)) * (each + kUnit);
-            if (units > 1 && time > 0.98 * best) continue;
-            best = time;
+        for (int64_t units = 1; units <= turns && pl.tokens_per_unit[i] == 1; units *= 2) {
+            const int64_t each = ceil_div(turns, units);
+            const double t = static_cast<double>(ceil_div(tokens * ceil_div(turns, each), share * pl.warps)) * (each + kUnit);
+            if (units > 1 && t > 0.98 * best) continue;
+            best = t;
             pl.heads_per_unit[i] = static_cast<int>(each) * rows;
         }
         pl.units_per_token[i] = static_cast<int>(ceil_div(heads[i], pl.heads_per_unit[i]));
-        pl.blocks[i] = static_cast<int>(std::min<int64_t>(share, ceil_div(tokens * pl.units_per_token[i], pl.warps)));
+        const int64_t units = ceil_div(tokens, pl.tokens_per_unit[i]) * pl.units_per_token[i];
+        pl.blocks[i] = static_cast<int>(std::min<int64_t>(share, ceil_div(units, pl.warps)));
     }
     return pl;
 }
 
-template <typename T, int kLanes, bool kPairs, bool kBwd, bool kMasked>
+template <typename T, int kLanes, bool kPairs, bool kBwd, bool kMasked, bool kAcross>
 cudaError_t rope_styled(const RopeParams& p, int blocks, cudaStream_t stream) {
     static std::atomic<uint64_t> allowed{0};
     constexpr int kBefore = kRopeBefore<kBwd, kMasked>, kAngle = kRopeWarps * 2 * static_cast<int>(sizeof(float));
-    const auto kernel = rope_kernel<T, kLanes, kPairs, kBwd, kMasked>;
+    const auto kernel = rope_kernel<T, kLanes, kPairs, kBwd, kMasked, kAcross>;
     const cudaError_t e = allow_dynamic_smem(reinterpret_cast<const void*>(kernel), kBefore + kAngle * rope_angles(kMaxPairs), allowed);
     if (e != cudaSuccess) return e;
     return launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kRopeThreads, kBefore + kAngle * rope_angles(p.rot / 2), 1, stream, p);
 }
-template <typename T, bool kBwd, bool kMasked>
+template <typename T, bool kBwd, bool kMasked, bool kAcross>
 cudaError_t rope_by_lanes(const RopeParams& p, int lanes, bool pairs, int blocks, cudaStream_t stream) {
     const auto run = [&](auto n) {
         constexpr int kLanes = decltype(n)::value;
-        return pairs ? rope_styled<T, kLanes, true, kBwd, kMasked>(p, blocks, stream) : rope_styled<T, kLanes, false, kBwd, kMasked>(p, blocks, stream);
+        return pairs ? rope_styled<T, kLanes, true, kBwd, kMasked, kAcross>(p, blocks, stream) : rope_styled<T, kLanes, false, kBwd, kMasked, kAcross>(p, blocks, stream);
     };
     switch (lanes) {
         case 2: return run(std::integral_constant<int, 2>());
@@ -688,8 +722,10 @@ cudaError_t rope_by_lanes(const RopeParams& p, int lanes, bool pairs, int blocks
 template <typename T, bool kBwd>
 cudaError_t rope_launch(const RopeParams& p, const RopePlan& pl, bool pairs, cudaStream_t stream) {
     const int blocks = pl.blocks[0] + pl.blocks[1];
-    if (pl.kind == RopePlan::kPieces) return rope_by_lanes<T, kBwd, false>(p, pl.lanes, pairs, blocks, stream);
-    if (pl.kind == RopePlan::kMasked) return rope_by_lanes<T, kBwd, true>(p, pl.lanes, pairs, blocks, stream);
+    const bool across = p.side[0].across || p.side[1].across;
+    if (pl.kind == RopePlan::kPieces)
+        return across ? rope_by_lanes<T, kBwd, false, true>(p, pl.lanes, pairs, blocks, stream) : rope_by_lanes<T, kBwd, false, false>(p, pl.lanes, pairs, blocks, stream);
+    if (pl.kind == RopePlan::kMasked) return rope_by_lanes<T, kBwd, true, false>(p, pl.lanes, pairs, blocks, stream);
     const size_t smem = sizeof(float) * kAnyWarps * (p.rot + (kBwd ? p.dim : 0));      // at most 32 KB
     const auto kernel = pairs ? rope_any_kernel<T, true, kBwd> : rope_any_kernel<T, false, kBwd>;
     return launch_beside(kernel, dim3(static_cast<unsigned>(blocks)), kAnyThreads, smem, 1, stream, p);

@@ -80,9 +80,18 @@ def test_dims(dtype, pairs, dim, rot):
 
 @pytest.mark.parametrize("dtype", DT)
 @pytest.mark.parametrize("layout", ["plain", "padded", "heads first", "odd"])
-@pytest.mark.parametrize("tokens,hq,hk", [(1, 1, 1), (1, 32, 8), (2, 5, 1), (37, 3, 3), (700, 8, 8), (33, 28, 4), (5, 0, 3), (6, 7, 0), (3000, 2, 1)])
+@pytest.mark.parametrize("tokens,hq,hk", [(1, 1, 1), (1, 32, 8), (2, 5, 1), (37, 3, 3), (700, 8, 8), (33, 28, 4), (5, 0, 3), (6, 7, 0), (3000, 2, 1), (1001, 1, 1), (777, 16, 1)])
 def test_layouts(dtype, layout, tokens, hq, hk):
     check(tokens, hq, hk, 64, 64, dtype, layout=layout)
+
+
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("dim,rot", [(32, 32), (64, 32), (128, 128), (66, 66), (100, 40), (20, 14)])
+def test_one_and_two_heads(dim, rot, pairs):
+    """Sides whose heads leave most of a warp's rows to other tokens."""
+    for dtype in DT:
+        check(203, 2, 1, dim, rot, dtype, pairs=pairs, positions="ends")
+        check(5, 9, 1, dim, rot, dtype, pairs=pairs, f32=True, eps=0.0)
 
 
 def test_many_tokens():
