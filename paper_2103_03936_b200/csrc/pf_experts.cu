@@ -169,10 +169,13 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) 
         const int e = e0 + threadIdx.x;
         int count = 0, below = 0;      // of all blocks, of those before this one
         if (e < E && kCluster) {
-            for (int b = 0; b < blocks; ++b) {
-                const int c = load_cluster(total + e, b);
-                if (b < rank) below += c;
-                count += c;
+            int c[kSortBlocks];      // (asked for all at once)
+#pragma unroll
+            for (int b = 0; b < kSortBlocks; ++b) c[b] = b < blocks ? load_cluster(total + e, b) : 0;
+#pragma unroll
+            for (int b = 0; b < kSortBlocks; ++b) {
+                if (b < rank) below += c[b];
+                count += c[b];
             }
         } else if (e < E) {
             below = total[e];
@@ -206,6 +209,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) 
             }
         }
     }
+    if (kCluster) asm volatile("barrier.cluster.arrive.release;" ::: "memory");      // this block has read the others' totals
     __syncthreads();
     // rows that no assignment takes
     const int thread = rank * kSortThreads + threadIdx.x, threads = blocks * kSortThreads;
@@ -237,7 +241,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) 
             }
         }
     }
-    if (kCluster) cluster_sync();      // (no block leaves while another reads its totals)
+    if (kCluster) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");        // (no block leaves while another reads its totals)
 }
 
 // ------------------------------------------------------------------------------ rows
@@ -339,6 +343,7 @@ struct RowParams {
 };
 
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
+constexpr int kWideThreads = 128, kWideWarps = kWideThreads / 32;      // of a block to a token
 constexpr int kRowsToClear = 4;      // rows of experts that the lanes of a token look at besides
 constexpr int kDispatchDeep = 4, kCombineDeep = 2;      // pieces of a row that a lane has in hand
 
@@ -476,7 +481,8 @@ __global__ void __launch_bounds__(kRowThreads) combine_kernel(const RowParams p)
 // dys[slot] = w dy[token], dw = <dy[token], ys[slot]> for kGroup experts of a token at a time (one by one where each row has its own pieces): kWide a block
 // to a token, else a group of lanes.
 template <typename T, int kUnit, bool kWide, int kGroup>
-__global__ void __launch_bounds__(kRowThreads) combine_bwd_kernel(const RowParams p) {
+__global__ void __launch_bounds__(kWide ? kWideThreads : kRowThreads) combine_bwd_kernel(const RowParams p) {
+    constexpr int kThreads = kWide ? kWideThreads : kRowThreads;
     using R = Rows<T, kUnit>;
     using P = typename R::P;
     constexpr int kN = P::kN, kDeep = kGroup == 4 ? 1 : 2;
@@ -484,9 +490,9 @@ __global__ void __launch_bounds__(kRowThreads) combine_bwd_kernel(const RowParam
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lanes = kWide ? 32 : p.lanes, lane = threadIdx.x & (lanes - 1), warp = threadIdx.x >> 5;
-    const int64_t item = (static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x) / lanes, token = kWide ? blockIdx.x : item;
-    const int start = kWide ? static_cast<int>(threadIdx.x) : lane, step = kWide ? kRowThreads : lanes;
-    __shared__ float red[kWide ? kRowWarps * kGroup : 1];
+    const int64_t item = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / lanes, token = kWide ? blockIdx.x : item;
+    const int start = kWide ? static_cast<int>(threadIdx.x) : lane, step = kWide ? kThreads : lanes;
+    __shared__ float red[kWide ? kWideWarps * kGroup : 1];
     if (kWide ? token < p.tokens : __any_sync(0xffffffffu, token < p.tokens)) {      // (all lanes of a warp take part in the sums)
         const bool there = token < p.tokens;
         const char* const dy = p.x + token * p.pitch;
@@ -560,7 +566,7 @@ __global__ void __launch_bounds__(kRowThreads) combine_bwd_kernel(const RowParam
                 __syncthreads();
                 if (threadIdx.x < kGroup && j0 + static_cast<int>(threadIdx.x) < p.k) {
                     float s = 0.f;
-                    for (int u = 0; u < kRowWarps; ++u) s += red[u * kGroup + threadIdx.x];
+                    for (int u = 0; u < kWideWarps; ++u) s += red[u * kGroup + threadIdx.x];
                     p.dweights[token * p.k + j0 + threadIdx.x] = s;
                 }
             } else if (there && lane == 0) {
@@ -612,7 +618,7 @@ cudaError_t rows_run(RowOp op, RowParams p, cudaStream_t stream) {
     p.lanes = pieces <= 8 ? 8 : pieces <= 16 ? 16 : 32;
     // (backward of combine) a block to a token where a warp to each would leave most of the machine idle
     const bool wide = op == kCombineBwd && p.tokens < num_sms() * kRowWarps * 2 && pieces > 32;
-    const int per_block = kRowThreads / p.lanes;
+    const int threads = wide ? kWideThreads : kRowThreads, per_block = threads / p.lanes;
     int64_t blocks = wide ? static_cast<int64_t>(p.tokens) : ceil_div(p.tokens, per_block), segments = 1;
     if (p.rows_out) blocks = std::max(blocks, ceil_div(p.rows, static_cast<int64_t>(kRowsToClear) * per_block));
     if (blocks == 0) return cudaSuccess;
@@ -629,7 +635,7 @@ cudaError_t rows_run(RowOp op, RowParams p, cudaStream_t stream) {
     } else {
         kernel = wide ? combine_bwd_kernel<T, kUnit, true, 1> : combine_bwd_kernel<T, kUnit, false, 1>;
     }
-    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(std::min<int64_t>(segments, 65535))), kRowThreads, 0, 1, stream, p);
+    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(std::min<int64_t>(segments, 65535))), threads, 0, 1, stream, p);
 }
 cudaError_t rows_launch(RowOp op, RowParams p, int unit, int64_t width, int dtype, cudaStream_t stream) {
     p.bytes = static_cast<int>(width * static_cast<int64_t>(dtype_size(dtype)));

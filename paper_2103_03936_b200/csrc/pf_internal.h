@@ -33,7 +33,7 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t dtype_size(int dtype) { return dtype == PF_BF16 ? 2 : 4; }
 
 // Checks of arguments that the entry points share.
-inline bool elem_aligned(const void* p, int dtype) { return (reinterpret_cast<uintptr_t>(p) % dtype_size(dtype)) == 0; }
+inline bool elem_aligned(const void* p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype_size(dtype) - 1)) == 0; }
 inline bool valid_dtype(int dtype) { return dtype == PF_F32 || dtype == PF_BF16; }
 inline int check_ws(const void* ws, size_t have, size_t need) {
     if (need == 0) return PF_OK;

@@ -512,16 +512,12 @@ struct AdamList {
 
 // Elements in front of the first one at which every array of tensor i is at its boundary.
 int head_of(const AdamList& l, int i) {
-    struct { const void* p; unsigned size, boundary; } arrays[5] = {
-        {l.p[i], static_cast<unsigned>(dtype_size(l.param_dtype)), 16}, {l.master ? l.master[i] : nullptr, 4, 16},
-        {l.g[i], static_cast<unsigned>(dtype_size(l.grad_dtype)), 16}, {l.m[i], l.state8 ? 1u : 4u, l.state8 ? 8u : 16u},
-        {l.v[i], l.state8 ? 1u : 4u, l.state8 ? 8u : 16u}};
-    for (int h = 0; h < (l.state8 ? 1 : kAdamVec); ++h) {
-        bool all = true;
-        for (const auto& a : arrays)      // (no masters: nothing to align)
-            if (a.p) all = all && (reinterpret_cast<uintptr_t>(a.p) + h * a.size) % a.boundary == 0;
-        if (all) return h;
-    }
+    const uintptr_t p = reinterpret_cast<uintptr_t>(l.p[i]), w = l.master ? reinterpret_cast<uintptr_t>(l.master[i]) : 0, g = reinterpret_cast<uintptr_t>(l.g[i]);
+    const uintptr_t m = reinterpret_cast<uintptr_t>(l.m[i]), v = reinterpret_cast<uintptr_t>(l.v[i]);
+    const size_t sp = dtype_size(l.param_dtype), sg = dtype_size(l.grad_dtype);
+    if (l.state8) return ((p | w | g) & 15) == 0 && ((m | v) & 7) == 0 ? 0 : kNoVectors;
+    for (size_t h = 0; h < kAdamVec; ++h)
+        if ((((p + h * sp) | (l.master ? w + h * 4 : 0) | (g + h * sg) | (m + h * 4) | (v + h * 4)) & 15) == 0) return static_cast<int>(h);
     return kNoVectors;
 }
 
