@@ -687,10 +687,10 @@ PyObject* qk_bwd(PyObject* const* a) {
     const unsigned flags = grad_flags(a[15], a[16]);
     const at::ScalarType wdt = (flags & PF_GRAD_F32) ? at::kFloat : any.scalar_type();
     if (truth(a[12])) {
-        if ((flags & PF_GRAD_ACCUMULATE) && ((r.q.defined() && r.wq.defined() && !dwq.defined()) || (r.k.defined() && r.wk.defined() && !dwk.defined())))
+        if ((flags & PF_GRAD_ACCUMULATE) && ((r.q_heads > 0 && r.wq.defined() && !dwq.defined()) || (r.k_heads > 0 && r.wk.defined() && !dwk.defined())))
             value_error("accumulate=True needs the dwq and dwk to add to");
-        if (!dwq.defined() && r.q.defined() && r.wq.defined()) dwq = empty({r.dim}, wdt, any);
-        if (!dwk.defined() && r.k.defined() && r.wk.defined()) dwk = empty({r.dim}, wdt, any);
+        if (!dwq.defined() && r.q_heads > 0 && r.wq.defined()) dwq = empty({r.dim}, wdt, any);
+        if (!dwk.defined() && r.k_heads > 0 && r.wk.defined()) dwk = empty({r.dim}, wdt, any);
     }
     on.check(dwq, "dwq", wdt, 1, true);
     on.check(dwk, "dwk", wdt, 1, true);

@@ -156,6 +156,16 @@ def test_no_tokens():
     assert (keep == 5).all() and (also == 6).all()
 
 
+def test_a_side_without_heads():
+    q, none, w, f = normal((9, 4, 64), torch.bfloat16, 1), torch.empty((9, 0, 64), dtype=torch.bfloat16, device="cuda"), normal((64,), torch.bfloat16, 2), frequencies(32)
+    a, b = pf.pf_qk_norm_rope_fwd(q, none, w, w, f)
+    assert b.shape == (9, 0, 64) and torch.equal(a, pf.pf_qk_norm_rope_fwd(q, None, w, None, f)[0])
+    dq, dk, dwq, dwk = pf.pf_qk_norm_rope_bwd(q, none, w, w, f, q, none)
+    assert dwk is None and dk.shape == (9, 0, 64)
+    want = pf.pf_qk_norm_rope_bwd(q, None, w, None, f, q, None)
+    assert torch.equal(dq, want[0]) and torch.equal(dwq, want[2])
+
+
 @pytest.mark.parametrize("dim,pairs", [(64, False), (64, True), (54, False)])
 def test_gradient_against_differences(dim, pairs):
     """<gradient, direction> of a weighted sum of the outputs against its central difference in 64 bits: the difference is off by
