@@ -340,12 +340,13 @@ struct RowParams {
     int tokens, k, rows;
     int bytes;                // of a row
     int lanes;                // of a warp to a token: 8, 16 or 32
+    int segments;             // blocks that share the rows of a block's tokens (dispatch)
 };
 
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
 constexpr int kWideThreads = 128, kWideWarps = kWideThreads / 32;      // of a block to a token
 constexpr int kRowsToClear = 4;      // rows of experts that the lanes of a token look at besides
-constexpr int kDispatchDeep = 4, kCombineDeep = 2;      // pieces of a row that a lane has in hand
+constexpr int kDispatchDeep = 4;      // pieces of a row that a lane has in hand
 
 // Clears those of four rows that no token has: pieces v0, v0 + step, ... of them.
 template <typename T, int kUnit>
@@ -367,7 +368,21 @@ __device__ __forceinline__ void clear_rows(const RowParams& p, int64_t item, int
     }
 }
 
-// xs[slot] = x[token], a group of lanes to a token; gridDim.y groups to a long row.
+// The block's place: its tokens, and its part of their rows.  Dispatch, which reads and writes whole rows, has the parts of a row beside one another,
+// so that what is in flight lies together (16384 x 2, 4096 wide: 75 us, 80 with the tokens' first parts together); combine, which gathers, the
+// tokens' first parts (58 us against 67).
+struct RowPlace {
+    int64_t block;
+    int segment;
+};
+template <bool kTogether>
+__device__ __forceinline__ RowPlace row_place(const RowParams& p) {
+    if constexpr (!kTogether) return {blockIdx.x, static_cast<int>(blockIdx.y)};
+    const unsigned b = blockIdx.x, n = static_cast<unsigned>(p.segments), q = n == 1 ? b : b / n;
+    return {q, static_cast<int>(b - q * n)};
+}
+
+// xs[slot] = x[token], a group of lanes to a token, several to a long row.
 template <typename T, int kUnit>
 __global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowParams p) {
     using R = Rows<T, kUnit>;
@@ -375,14 +390,15 @@ __global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowParams p
     constexpr int kDeep = R::kAligned ? kDispatchDeep : 2;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & (p.lanes - 1), step = gridDim.y * p.lanes * kDeep;
-    const int64_t item = (static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x) / p.lanes;
+    const RowPlace place = row_place<true>(p);
+    const int lane = threadIdx.x & (p.lanes - 1), step = p.segments * p.lanes * kDeep;
+    const int64_t item = (place.block * kRowThreads + threadIdx.x) / p.lanes;
     if (item < p.tokens) {
         const char* const from = p.x + item * p.pitch;
         const int* const slots = p.slots + item * p.k;
         if constexpr (R::kAligned) {      // read once
             const int n = p.bytes / R::kBytes;
-            for (int v0 = blockIdx.y * p.lanes * kDeep + lane; v0 < n; v0 += step) {
+            for (int v0 = place.segment * p.lanes * kDeep + lane; v0 < n; v0 += step) {
                 P d[kDeep];
 #pragma unroll
                 for (int u = 0; u < kDeep; ++u)
@@ -403,7 +419,7 @@ __global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowParams p
                 if (slot < 0 || slot >= p.rows) continue;
                 char* const to = p.rows_out + slot * p.out_pitch;
                 const int n = R::pieces(to, p.bytes);
-                for (int v0 = blockIdx.y * p.lanes * kDeep + lane; v0 < n; v0 += step) {
+                for (int v0 = place.segment * p.lanes * kDeep + lane; v0 < n; v0 += step) {
                     P d[kDeep];
 #pragma unroll
                     for (int u = 0; u < kDeep; ++u)
@@ -415,23 +431,25 @@ __global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowParams p
             }
         }
     }
-    clear_rows<T, kUnit>(p, item, blockIdx.y * p.lanes + lane, gridDim.y * p.lanes);
+    clear_rows<T, kUnit>(p, item, place.segment * p.lanes + lane, p.segments * p.lanes);
 }
 
-// y[token] = sum_j w_j rows_in[slot_j], kGroup experts of a token at a time.
-template <typename T, int kUnit, int kGroup>
+// y[token] = sum_j w_j rows_in[slot_j], kGroup experts of a token and kDeep pieces of a lane at a time (two of 16 bytes: 16384 x 2, 4096
+// wide: 58 us, with four 69, with one 74; four of 8 or 4 bytes: 8192 x 2, 1002 wide: 16 us, with two 19).
+template <typename T, int kUnit, int kGroup, int kDeep>
 __global__ void __launch_bounds__(kRowThreads) combine_kernel(const RowParams p) {
     using R = Rows<T, kUnit>;
     using P = typename R::P;
-    constexpr int kDeep = kCombineDeep, kN = P::kN;
+    constexpr int kN = P::kN;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const RowPlace place = row_place<false>(p);
     const int lane = threadIdx.x & (p.lanes - 1);
-    const int64_t token = (static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x) / p.lanes;
+    const int64_t token = (place.block * kRowThreads + threadIdx.x) / p.lanes;
     if (token >= p.tokens) return;
     char* const y = p.y + token * p.pitch;
     const int n = R::pieces(y, p.bytes);
-    for (int v0 = blockIdx.y * p.lanes * kDeep + lane; v0 < n; v0 += gridDim.y * p.lanes * kDeep) {
+    for (int v0 = place.segment * p.lanes * kDeep + lane; v0 < n; v0 += static_cast<int>(gridDim.y) * p.lanes * kDeep) {
         float sum[kDeep][kN];
 #pragma unroll
         for (int u = 0; u < kDeep; ++u)
@@ -627,15 +645,20 @@ cudaError_t rows_run(RowOp op, RowParams p, cudaStream_t stream) {
         kernel = dispatch_kernel<T, kUnit>;
         segments = ceil_div(pieces, 32 * kDispatchDeep);
     } else if (op == kCombine) {
-        kernel = p.k == 1 ? combine_kernel<T, kUnit, 1> : p.k == 2 ? combine_kernel<T, kUnit, 2> : combine_kernel<T, kUnit, 4>;
-        segments = ceil_div(pieces, 32 * kCombineDeep);
+        constexpr int kDeep = Rows<T, kUnit>::kBytes == 16 ? 2 : 4;
+        kernel = p.k == 1 ? combine_kernel<T, kUnit, 1, kDeep> : p.k == 2 ? combine_kernel<T, kUnit, 2, kDeep> : combine_kernel<T, kUnit, 4, 2>;
+        segments = ceil_div(pieces, 32 * (p.k <= 2 ? kDeep : 2));
     } else if constexpr (kAligned) {
         kernel = wide ? (p.k == 1 ? combine_bwd_kernel<T, kUnit, true, 1> : p.k == 2 ? combine_bwd_kernel<T, kUnit, true, 2> : combine_bwd_kernel<T, kUnit, true, 4>)
                       : (p.k == 1 ? combine_bwd_kernel<T, kUnit, false, 1> : p.k == 2 ? combine_bwd_kernel<T, kUnit, false, 2> : combine_bwd_kernel<T, kUnit, false, 4>);
     } else {
         kernel = wide ? combine_bwd_kernel<T, kUnit, true, 1> : combine_bwd_kernel<T, kUnit, false, 1>;
     }
-    return launch_beside(kernel, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(std::min<int64_t>(segments, 65535))), threads, 0, 1, stream, p);
+    if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
+    segments = std::min<int64_t>(segments, op == kDispatch ? 0x7fffffffLL / blocks : 65535);
+    p.segments = static_cast<int>(segments);
+    const dim3 grid = op == kDispatch ? dim3(static_cast<unsigned>(blocks * segments)) : dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(segments));
+    return launch_beside(kernel, grid, threads, 0, 1, stream, p);
 }
 cudaError_t rows_launch(RowOp op, RowParams p, int unit, int64_t width, int dtype, cudaStream_t stream) {
     p.bytes = static_cast<int>(width * static_cast<int64_t>(dtype_size(dtype)));
