@@ -571,7 +571,8 @@ template <int kParam, typename G>
 cudaError_t adamw_sized(const AdamList& l, const AdamHyper& h, cudaStream_t stream) {
     // (short lists have tables of their own, as in pf_pack.cu: a launch copies all of it, 31 KB for 448 tensors)
     if (l.count <= 16) return adamw_by<16, kParam, G>(l, h, stream);
-    if (l.count <= 96) return adamw_by<96, kParam, G>(l, h, stream);
+    if (l.count <= 64) return adamw_by<64, kParam, G>(l, h, stream);
+    if (l.count <= 192) return adamw_by<192, kParam, G>(l, h, stream);
     return adamw_by<448, kParam, G>(l, h, stream);
 }
 template <int kParam>
