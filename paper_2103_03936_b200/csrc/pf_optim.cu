@@ -403,31 +403,34 @@ struct StateBlock {
         const int field_m = scale_field<E4M3>(most_m), field_v = scale_field<E5M2>(most_v);
         const F2 over_m = both(__int_as_float((254 - field_m) << 23)), over_v = both(__int_as_float((254 - field_v) << 23));      // 1 / scale
         const uint32_t least_v = static_cast<uint32_t>(field_v - 14) << 23;      // e5m2's smallest normal number, 2^-14
-        // (few blocks have a v that small, or none: without one the rounded values need no limit)
-        const bool small_v = __any_sync(0xffffffffu, low_v < least_v);
         const F2 down = both(0x1p-120f), up = both(0x1p120f), zero = both(0.f);
         const uint32_t beyond = key + static_cast<uint32_t>(beg >> 32) * kBeyond32;      // (a block lies on one side of 2^32)
         const uint32_t first = ((static_cast<uint32_t>(beg) + static_cast<uint32_t>(lane) * 8) ^ (beyond & ~7u)) * kFirstRound;
+        uint32_t zm[8], zv[8];
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            const float2 x = split(fm[n / 2]), y = split(fv[n / 2]);
+            // (eight places from a multiple of eight on differ from the key in three bits apart from the others, so the product is a sum)
+            const uint32_t start = kVectors ? first + ((beyond & 7u) ^ n) * kFirstRound
+                                            : ((static_cast<uint32_t>(beg) + static_cast<uint32_t>(place(lane, n))) ^ beyond) * kFirstRound;
+            const uint32_t r = random_bits(start), upper = r >> 16;
+            zm[n] = rounded<E4M3>(__float_as_uint(n % 2 ? x.y : x.x), (r ^ upper) & 0xffffu);
+            zv[n] = rounded<E5M2>(__float_as_uint(n % 2 ? y.y : y.x), upper);
+        }
+        // (few blocks have a v that small, or none: without one the rounded values need no limit)
+        if (__any_sync(0xffffffffu, low_v < least_v)) {
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                const float2 y = split(fv[n / 2]);
+                zv[n] = max(zv[n], min(__float_as_uint(n % 2 ? y.y : y.x), 1u) * least_v);
+            }
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float2 x = split(fm[e]), y = split(fv[e]);
-            uint32_t zm[2], zv[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int n = 2 * e + i;
-                // (eight places from a multiple of eight on differ from the key in three bits apart from the others, so the product is a sum)
-                const uint32_t start = kVectors ? first + ((beyond & 7u) ^ n) * kFirstRound
-                                                : ((static_cast<uint32_t>(beg) + static_cast<uint32_t>(place(lane, n))) ^ beyond) * kFirstRound;
-                const uint32_t r = random_bits(start), upper = r >> 16;
-                const uint32_t bits_m = __float_as_uint(i ? x.y : x.x), bits_v = __float_as_uint(i ? y.y : y.x);
-                zm[i] = rounded<E4M3>(bits_m, (r ^ upper) & 0xffffu);
-                zv[i] = rounded<E5M2>(bits_v, upper);
-                if (small_v) zv[i] = max(zv[i], min(bits_v, 1u) * least_v);
-            }
             // m below e4m3's smallest normal number, 2^-6, becomes zero: that is 2^-126 in between (and minus zero plus zero is zero)
-            const F2 sm = mul2(f2(__uint_as_float(zm[0]), __uint_as_float(zm[1])), over_m);
+            const F2 sm = mul2(f2(__uint_as_float(zm[2 * e]), __uint_as_float(zm[2 * e + 1])), over_m);
             fm[e] = fma2(mul2_flush(sm, down), up, zero);
-            fv[e] = mul2(f2(__uint_as_float(zv[0]), __uint_as_float(zv[1])), over_v);
+            fv[e] = mul2(f2(__uint_as_float(zv[2 * e]), __uint_as_float(zv[2 * e + 1])), over_v);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
