@@ -4,6 +4,7 @@ import torch
 
 import _ops
 import paper_2103_03936_b200 as pf
+from _gpu import Scratch
 
 pytestmark = pytest.mark.gpu
 DT = [torch.bfloat16, torch.float32]
@@ -50,6 +51,18 @@ def test_sort(tokens, k, experts, capacity):
         got = sorted_rows(ids, experts, capacity)
         for g, w, name in zip(got, _ops.sort(ids.tolist(), experts, capacity), ("slots", "sources", "counts", "offsets")):
             assert g.reshape(-1).tolist() == w, name
+
+
+@pytest.mark.parametrize("tokens,k,experts", [(32769, 1, 2048), (200001, 1, 5), (60000, 8, 256)])
+def test_a_workspace_of_the_queried_size(tokens, k, experts):
+    ids = choose(tokens, k, experts, 4).cuda()
+    scratch = Scratch(pf.pf_expert_sort_workspace(tokens, k, experts))
+    got = pf.pf_expert_sort(ids, experts, workspace=scratch.t)
+    scratch.check()
+    order = torch.sort(ids.flatten(), stable=True).indices
+    assert torch.equal(got[1].long(), order) and torch.equal(got[0].flatten().long()[order], torch.arange(tokens * k, device="cuda"))
+    for a, b in zip(got, pf.pf_expert_sort(ids, experts)):
+        assert torch.equal(a, b)
 
 
 def test_sort_of_one_expert_and_of_none():

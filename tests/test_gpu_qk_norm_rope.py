@@ -4,6 +4,7 @@ import torch
 
 import _ops
 import paper_2103_03936_b200 as pf
+from _gpu import Scratch
 
 pytestmark = pytest.mark.gpu
 DT = [torch.bfloat16, torch.float32]
@@ -154,6 +155,16 @@ def test_no_tokens():
     keep, also = torch.full((64,), 5.0, device="cuda"), torch.full((64,), 6.0, device="cuda")
     pf.pf_qk_norm_rope_bwd(q, q, w, w, f, q, q, dwq=keep, dwk=also, accumulate=True)
     assert (keep == 5).all() and (also == 6).all()
+
+
+@pytest.mark.parametrize("tokens,hq,hk,dim", [(3, 1, 1, 64), (5000, 8, 1, 64), (9000, 32, 8, 128), (4000, 3, 3, 66), (3000, 2, 2, 600)])
+def test_a_workspace_of_the_queried_size(tokens, hq, hk, dim):
+    q, k, w, f = normal((tokens, hq, dim), torch.bfloat16, 1), normal((tokens, hk, dim), torch.bfloat16, 2), normal((dim,), torch.bfloat16, 3), frequencies(dim // 2)
+    scratch = Scratch(pf.pf_qk_norm_rope_bwd_workspace(tokens, hq, hk, dim))
+    got = pf.pf_qk_norm_rope_bwd(q, k, w, w, f, q, k, workspace=scratch.t)
+    scratch.check()
+    for a, b in zip(got, pf.pf_qk_norm_rope_bwd(q, k, w, w, f, q, k)):
+        assert torch.equal(a, b)
 
 
 def test_a_side_without_heads():
