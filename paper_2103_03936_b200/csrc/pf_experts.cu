@@ -711,7 +711,8 @@ int pf_expert_sort(const int32_t* ids, int64_t tokens, int k, int experts, int64
     const auto kernel = cluster ? sort_kernel<true> : sort_kernel<false>;
     const size_t each = sizeof(int) * (kSortWarps + 3);      // of shared memory for an expert: 152 KB for the most of them
     static std::atomic<uint64_t> allowed[2];
-    if (each * experts > 48 * 1024) PF_CUDA(allow_dynamic_smem(reinterpret_cast<const void*>(kernel), each * kMostExperts, allowed[cluster ? 1 : 0]));
+    // (48 KB without asking, of which the kernel's own array takes a part)
+    if (each * experts > 47 * 1024) PF_CUDA(allow_dynamic_smem(reinterpret_cast<const void*>(kernel), each * kMostExperts, allowed[cluster ? 1 : 0]));
     const dim3 grid(static_cast<unsigned>(blocks));
     if (!cluster) PF_CUDA(launch_beside(count_kernel, grid, kSortThreads, sizeof(int) * experts, 1, stream, p));
     PF_CUDA(launch_beside(kernel, grid, kSortThreads, each * experts, cluster ? blocks : 1, stream, p));

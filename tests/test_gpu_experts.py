@@ -1,4 +1,8 @@
 """GPU parity of the experts' sort, dispatch and combine against plain forms in 64 bits."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -63,6 +67,20 @@ def test_a_workspace_of_the_queried_size(tokens, k, experts):
     assert torch.equal(got[1].long(), order) and torch.equal(got[0].flatten().long()[order], torch.arange(tokens * k, device="cuda"))
     for a, b in zip(got, pf.pf_expert_sort(ids, experts)):
         assert torch.equal(a, b)
+
+
+def test_sort_where_shared_memory_reaches_48_kb():
+    """Numbers of experts around those at which a block needs more than 48 KB, in a process that has not sorted for more of them."""
+    code = """
+import torch, paper_2103_03936_b200 as pf
+for tokens in (500, 20000):
+    for experts in (640, *range(643, 650)):
+        ids = torch.randint(experts, (tokens, 2), dtype=torch.int32, device="cuda")
+        order = pf.pf_expert_sort(ids, experts)[1]
+        assert torch.equal(order.long(), torch.sort(ids.flatten(), stable=True).indices), (tokens, experts)
+"""
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert done.returncode == 0, done.stderr
 
 
 def test_sort_of_one_expert_and_of_none():
