@@ -354,7 +354,7 @@ int pf_unpack_factor_grads(const void* flat, int64_t flat_elems, void* const* gr
  *   offsets [experts + 1] int32  first row of each expert; behind the last, experts * capacity or the rows in use
  * One launch and no workspace up to 32768 assignments; two launches and pf_expert_sort_workspace bytes beyond.  PF_ERR_UNSUPPORTED: more than
  * 2048 experts, or 2^30 assignments or rows.
- * pf_expert_rows returns `rows` (0 for invalid sizes).
+ * pf_expert_rows returns `rows` (0 for sizes that pf_expert_sort refuses).
  *
  * The other four take slots and sources as pf_expert_sort left them (an index outside the rows counts as none) and
  * matrices of `width` columns at any pitch; x, y, dx, dy have `tokens` rows, xs, ys, dxs, dys `rows`:

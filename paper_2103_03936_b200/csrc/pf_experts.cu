@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) 
             below = total[e];
             count = chosen[e];
         }
-        int row = e * p.capacity;
+        int row = e < E ? e * p.capacity : 0;
         if (p.capacity == 0) {
             int x = count;
 #pragma unroll
@@ -620,6 +620,12 @@ int check_sizes(int64_t tokens, int k, int64_t rows, int64_t width, int dtype) {
     return PF_OK;
 }
 
+int check_assignments(int64_t tokens, int k, int experts, int64_t capacity) {
+    if (tokens < 0 || k < 1 || experts < 1 || capacity < 0) return PF_ERR_INVALID_ARG;
+    if (k > (1 << 16) || tokens > (1LL << 30) / k || experts > kMostExperts || capacity > (1LL << 30) / experts) return PF_ERR_UNSUPPORTED;
+    return PF_OK;
+}
+
 // Blocks of a sort: a cluster's (1, 2, 4 or 8), or more of them.
 int sort_blocks(int64_t assignments) {
     if (assignments > kClusterMost) return static_cast<int>(std::max<int64_t>(kSortBlocks + 1, std::min<int64_t>(num_sms(), ceil_div(assignments, 4 * kSortThreads))));
@@ -685,20 +691,20 @@ using namespace pf;
 extern "C" {
 
 int64_t pf_expert_rows(int64_t tokens, int k, int experts, int64_t capacity) {
-    if (tokens < 0 || k < 1 || experts < 1 || capacity < 0) return 0;
+    if (check_assignments(tokens, k, experts, capacity) != PF_OK) return 0;
     return capacity > 0 ? experts * capacity : tokens * k;
 }
 
 size_t pf_expert_sort_workspace(int64_t tokens, int k, int experts) {
-    if (tokens < 0 || k < 1 || experts < 1 || k > (1 << 16) || tokens > (1LL << 30) / k || experts > kMostExperts) return 0;
+    if (check_assignments(tokens, k, experts, 0) != PF_OK) return 0;
     const int blocks = sort_blocks(tokens * k);
     return blocks > kSortBlocks ? align_up(sizeof(int) * static_cast<size_t>(blocks) * experts, 256) : 0;
 }
 
 int pf_expert_sort(const int32_t* ids, int64_t tokens, int k, int experts, int64_t capacity, int32_t* slots, int32_t* sources, int32_t* counts,
                    int32_t* offsets, void* workspace, size_t workspace_bytes, void* cuda_stream) {
-    if (tokens < 0 || k < 1 || experts < 1 || capacity < 0) return PF_ERR_INVALID_ARG;
-    if (k > (1 << 16) || tokens > (1LL << 30) / k || experts > kMostExperts || capacity > (1LL << 30) / experts) return PF_ERR_UNSUPPORTED;
+    const int sizes = check_assignments(tokens, k, experts, capacity);
+    if (sizes != PF_OK) return sizes;
     const int64_t a = tokens * k, rows = pf_expert_rows(tokens, k, experts, capacity);
     if (!list_valid(ids, a) || !list_valid(slots, a) || !list_valid(sources, rows) || !list_valid(counts, 1) || !list_valid(offsets, 1))
         return PF_ERR_INVALID_ARG;

@@ -258,6 +258,15 @@ def test_on_another_stream():
     assert torch.equal(xs, want)
 
 
+def test_a_capacity_that_is_refused_takes_no_memory():
+    ids = choose(10, 2, 4, 1).cuda()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    with pytest.raises(pf.PfError) as e:
+        pf.pf_expert_sort(ids, 4, capacity=1 << 29)
+    assert e.value.status == 2 and torch.cuda.max_memory_allocated() - before < 1 << 20
+
+
 def test_refusals():
     ids = choose(10, 2, 3, 1).cuda()
     slots, sources, _, _ = pf.pf_expert_sort(ids, 3)

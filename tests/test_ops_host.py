@@ -24,6 +24,13 @@ def test_rows():
     assert pf.pf_expert_rows(-1, 2, 4) == 0 and pf.pf_expert_rows(10, 0, 4) == 0 and pf.pf_expert_rows(10, 2, 4, -1) == 0
 
 
+def test_rows_of_refused_sizes():
+    """None, so that a caller who sizes `sources` by them asks for no memory (or for a product that wrapped)."""
+    for sizes in ((10, 2, 4, 1 << 29), (10, 2, 2048, 1 << 62), (1 << 30, 2, 4, 0), (1 << 62, 4, 4, 0), (10, 2, 2049, 0), (10, (1 << 16) + 1, 4, 0)):
+        assert pf.pf_expert_rows(*sizes) == 0, sizes
+    assert pf.pf_expert_rows(1 << 29, 2, 4) == 1 << 30 and pf.pf_expert_rows(1, 1, 4, 1 << 28) == 1 << 30
+
+
 def test_sort_refuses(L):
     def call(**kw):
         a = dict(ids=P, tokens=10, k=2, experts=4, capacity=0, slots=P, sources=P, counts=P, offsets=P, ws=0, wsb=0, stream=0) | kw
