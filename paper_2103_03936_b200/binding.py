@@ -324,6 +324,8 @@ def pf_qk_norm_rope_bwd(q, k, wq, wk, inv_freq, dq_out, dk_out, *, positions=Non
 def pf_adamw_scalars(*, lr, betas=(0.9, 0.999), step, grad_scale=1.0, seed=0):
     """The five values that replace lr, step, grad_scale and seed of a pf_adamw_step with scalars=: a float32 tensor on the host
     (the seed's bits in the last), to be copied into the device tensor that the step reads."""
+    if step < 1 or not 0 <= seed < 1 << 32:
+        raise ValueError("need a step from 1 on and a seed of 0 .. 2^32 - 1")
     t = torch.tensor([lr, 1 - betas[0] ** step, 1 - betas[1] ** step, grad_scale, 0], dtype=torch.float32)
     t.view(torch.int32)[4] = seed - (1 << 32) if seed >= 1 << 31 else seed
     return t

@@ -161,6 +161,13 @@ def test_scalars_of_a_replayed_step():
     assert int(t.view(torch.int32)[4]) == -2 and int(pf.pf_adamw_scalars(lr=1.0, step=1, seed=5).view(torch.int32)[4]) == 5
 
 
+def test_scalars_refuse_what_the_step_refuses():
+    """Step 0 has corrections of zero, which would make every parameter infinite."""
+    for bad in (dict(step=0), dict(step=-1), dict(step=1, seed=-1), dict(step=1, seed=1 << 32)):
+        with pytest.raises(ValueError):
+            pf.pf_adamw_scalars(lr=1e-3, **bad)
+
+
 @pytest.mark.parametrize("e4m3", [True, False])
 def test_rounding_of_states_is_fair(e4m3):
     """Mean of what a value is rounded to over the random bits of many places and seeds: the value itself, to the spread of the mean
