@@ -362,7 +362,7 @@ int pf_unpack_factor_grads(const void* flat, int64_t flat_elems, void* const* gr
  *   dispatch_bwd   dx[t]  = sum over j of dxs[slots[t, j]]
  *   combine_fwd    y[t]   = sum over j of weights[t, j] ys[slots[t, j]]                weights [tokens, k] fp32, NULL = ones
  *   combine_bwd    dys[slots[t, j]] = weights[t, j] dy[t], other rows zeroed;  dweights[t, j] = <dy[t], ys[slots[t, j]]>, 0 without a row
- *                  (dys or dweights may be NULL: not wanted)
+ *                  (dys or dweights may be NULL: not wanted; weights may not: the gradient of a sum without weights is dispatch_fwd of dy)
  * Sums run over j in order, in fp32, and are rounded once; assignments without a row add nothing, so a token all of whose
  * assignments were dropped gives zeros.  dweights is fp32.  What rows without an assignment hold is never read.  One launch each, no workspace.
  * ------------------------------------------------------------------------------- */
