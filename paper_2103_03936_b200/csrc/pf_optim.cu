@@ -454,6 +454,10 @@ struct StateBlock {
     }
 };
 
+// Pieces of a thread at a time: two where all is in 16 bits and less (26.8 M elements: 51 us, with one 59); parameters read in fp32 have enough under
+// way with one (15.1 M with masters: 41.0 us, with two 43.7; 17.3 M of fp32: 45.2 and 46.7).
+template <int kParam> constexpr int kAdam8Deep = kParam == P_BF16 ? kAdamDeep : 1;
+
 template <int kMost, int kParam, typename G>
 __global__ void __launch_bounds__(kAdamThreads, 4) adamw8_kernel(const __grid_constant__ AdamTable<kMost> tb, const AdamHyper hyper) {
     const int chunk = blockIdx.x, t = tensor_of(tb, chunk), local = chunk - tb.chunk_prefix[t];
@@ -471,14 +475,15 @@ __global__ void __launch_bounds__(kAdamThreads, 4) adamw8_kernel(const __grid_co
     const int64_t beg = static_cast<int64_t>(local) * tb.steps * kAdamPiece + warp * kStateBlock;
     // The scales of a block's pieces are stored together in the end: one by one they are parts of 32-byte sectors that other warps still read, which
     // kept those waiting (26.8 M elements: 57 us, 93 with half of the loads in flight; 53 without the stores).
-    __shared__ float2 scales[kAdamDeep][kAdamWarps];
+    constexpr int kDeep = kAdam8Deep<kParam>;
+    __shared__ float2 scales[kDeep][kAdamWarps];
     if (tb.head[t] == 0 && beg + (tb.steps - 1) * kAdamPiece + kStateBlock <= n) {      // whole blocks, all on the way at once
-        StateBlock<kParam, G, true> b[kAdamDeep];
+        StateBlock<kParam, G, true> b[kDeep];
 #pragma unroll
-        for (int u = 0; u < kAdamDeep; ++u)
+        for (int u = 0; u < kDeep; ++u)
             if (u < tb.steps) b[u].load(a, mc, vc, msc, vsc, beg + u * kAdamPiece, kStateBlock, lane);
 #pragma unroll
-        for (int u = 0; u < kAdamDeep; ++u)
+        for (int u = 0; u < kDeep; ++u)
             if (u < tb.steps) b[u].step(hp, a, mc, vc, scales[u][warp], beg + u * kAdamPiece, kStateBlock, lane, key);
     } else {
 #pragma unroll 1
@@ -531,7 +536,7 @@ cudaError_t adamw_by(const AdamList& l, const AdamHyper& h, cudaStream_t stream)
     for (int i = 0; i < l.count; ++i) pieces += ceil_div(l.n[i], kAdamPiece);
     // a block takes several pieces where enough blocks are left for every SM
     const int64_t fill = static_cast<int64_t>(num_sms()) * kAdamFill;
-    const int steps = pieces >= kAdamDeep * fill ? kAdamDeep : 1;
+    const int deep = l.state8 ? kAdam8Deep<kParam> : kAdamDeep, steps = pieces >= deep * fill ? deep : 1;
     int i = 0;
     while (i < l.count) {
         AdamTable<kMost> tb;
