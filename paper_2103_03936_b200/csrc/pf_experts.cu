@@ -124,7 +124,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) 
         for (int i = 0; i < kHeld; ++i) {
             const int a = a0 + 32 * i + lane;
             held[i] = a < end ? p.ids[a] : -1;
-            if (held[i] >= E) held[i] = -1;
+            // (another negative id could have an expert's lowest bits, which are all that the ballots compare)
+            if (static_cast<unsigned>(held[i]) >= static_cast<unsigned>(E)) held[i] = -1;
         }
     };
     for (int a0 = beg; a0 < end; a0 += 32 * kHeld) {

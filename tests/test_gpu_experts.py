@@ -288,3 +288,23 @@ def test_refusals():
     assert e.value.status == 2
     with pytest.raises(pf.PfError):
         pf.pf_expert_combine_bwd(ys, slots, sources, w, x, need_dys=False, need_dweights=False)
+
+
+@pytest.mark.parametrize("tokens,k,experts,capacity", [
+    (3, 1, 2, 0), (40, 1, 2, 0), (20, 2, 8, 0), (511, 2, 64, 20), (1111, 3, 61, 0), (2000, 8, 256, 70), (777, 5, 513, 0), (5000, 4, 2048, 12), (1, 2, 1, 1),
+    (40000, 1, 7, 0), (33000, 2, 64, 900), (50001, 3, 2048, 70), (32769, 1, 1, 0)])
+def test_any_id_outside_the_experts_gets_no_row(tokens, k, experts, capacity):
+    """Negative ids of every kind (those whose low bits are an expert's among them) and those beyond the last, alone and in front of all of 32."""
+    g = torch.Generator().manual_seed(11)
+    bits, low = experts.bit_length(), -(1 << 31)
+    pool = [-1, -2, -8, -29, -100, low, low + 1, low + experts - 1, experts, experts + 1, (1 << 31) - 1]
+    pool += [-(1 << b) + e for b in (bits, bits + 1, bits + 4, 20, 30) for e in (0, experts // 2, experts - 1)]
+    pool = torch.tensor(sorted({i for i in pool if not 0 <= i < experts}))
+    for share in (0.1, 0.6):
+        ids = torch.randint(0, experts, (tokens * k,), generator=g)
+        out = torch.rand(tokens * k, generator=g) < share
+        out[::32] = True
+        ids = torch.where(out, pool[torch.randint(0, len(pool), (tokens * k,), generator=g)], ids).to(torch.int32).view(tokens, k)
+        got = sorted_rows(ids, experts, capacity)
+        for a, w, name in zip(got, _ops.sort(ids.tolist(), experts, capacity), ("slots", "sources", "counts", "offsets")):
+            assert a.reshape(-1).tolist() == w, name
