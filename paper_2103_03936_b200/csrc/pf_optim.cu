@@ -432,6 +432,15 @@ struct StateBlock {
             fm[e] = fma2(mul2_flush(sm, down), up, zero);
             fv[e] = mul2(f2(__uint_as_float(zv[2 * e]), __uint_as_float(zv[2 * e + 1])), over_v);
         }
+        // (a value of fp32's highest binade that is rounded up is an infinity in between, and 256 or 2^15 as a code)
+        if (field_m == 254 - E4M3::kTop || field_v == 254 - E5M2::kTop) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 x = split(fm[e]), y = split(fv[e]);
+                fm[e] = f2(fmaxf(fminf(x.x, 256.f), -256.f), fmaxf(fminf(x.y, 256.f), -256.f));
+                fv[e] = f2(fminf(y.x, 0x1p15f), fminf(y.y, 0x1p15f));
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             m[i] = encode4<__NV_E4M3>(fm[2 * i], fm[2 * i + 1]) | nan_m[i];

@@ -176,6 +176,36 @@ def test_8bit_states_of_odd_gradients():
     check8(t, old, sizes, False, H, 5)
 
 
+def test_8bit_states_at_the_top_of_fp32():
+    """Values of the highest binade are rounded up to the code of 2^128, and are not infinite; what follows from the codes is finite.
+
+    beta = 0 makes m the gradient and v its square: the first four blocks overflow v in fp32, the others have v near its end."""
+    sizes = [256 * 8 + 100]
+    t, _ = state8(sizes, torch.float32, torch.float32, False, "own", 0, 3)
+    for name in ("m", "v", "m_scales", "v_scales"):
+        t[name][0].view(torch.uint8).zero_()
+    g = t["grads"][0]
+    g[:1024] = 3.38e38
+    g[256:512:3] *= -1
+    g[512:1024:5] = -1e30
+    g[1024:] = 1.842e19
+    g[1100::7] = -1.7e19
+    g[2048:2060] = 1e10
+    h = H | {"betas": (0.0, 0.0), "step": 1, "grad_scale": 1.0}
+    old = t["grads"][0].cpu()
+    pf.pf_adamw_step(**t, **h, seed=5)
+    m, v = _ops.moments32(old, torch.zeros(sizes[0]), torch.zeros(sizes[0]), h["betas"])
+    bits = _ops.noise(sizes[0], 5, 0)
+    for s, value, half in (("m", m, bits & 0xFFFF), ("v", v, bits >> 16)):
+        codes, scales = _ops.encode(value, half, s == "m")
+        assert torch.equal(t[s][0].cpu().view(torch.uint8), codes.view(torch.uint8)), s
+        assert torch.equal(t[s + "_scales"][0].cpu(), scales), s
+    assert (t["m"][0][:256].float() == 256).sum() > 100 and (t["v"][0][1024:].float() == 2.0 ** 15).sum() > 100
+    t["grads"][0].zero_()
+    pf.pf_adamw_step(**t, **H, seed=6)
+    assert torch.isfinite(t["m"][0].float()).all() and torch.isfinite(t["v"][0][1024:].float()).all()
+
+
 def test_what_is_not_finite_stays_where_it_is():
     for eight in (False, True):
         make = state8 if eight else lists
