@@ -94,6 +94,9 @@ Workspace workspace(PyObject* o, size_t need, const at::Tensor& like, const Stre
     Workspace w;
     if (o != Py_None) {
         w.given = tensor(o, "workspace");
+        // (of a strided or expanded one the kernels would use memory that is not its)
+        if (!w.given.is_cuda() || w.given.device() != like.device() || !w.given.is_contiguous())
+            value_error("workspace: need a contiguous CUDA tensor on the device of the other tensors");
         w.p = w.given.data_ptr();
         w.bytes = static_cast<size_t>(w.given.numel());
         return w;

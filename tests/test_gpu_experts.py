@@ -308,3 +308,20 @@ def test_any_id_outside_the_experts_gets_no_row(tokens, k, experts, capacity):
         got = sorted_rows(ids, experts, capacity)
         for a, w, name in zip(got, _ops.sort(ids.tolist(), experts, capacity), ("slots", "sources", "counts", "offsets")):
             assert a.reshape(-1).tolist() == w, name
+
+
+def test_a_workspace_that_is_no_whole_buffer_on_the_device_is_refused():
+    ids = choose(40000, 1, 64, 1).cuda()
+    need = pf.pf_expert_sort_workspace(40000, 1, 64)
+    for room in (torch.empty(need, dtype=torch.uint8), torch.empty(2 * need, dtype=torch.uint8, device="cuda")[::2],
+                 torch.empty(1, dtype=torch.uint8, device="cuda").expand(need)):
+        with pytest.raises(ValueError, match="workspace"):
+            pf.pf_expert_sort(ids, 64, workspace=room)
+        x = torch.zeros(8, 8, device="cuda")
+        with pytest.raises(ValueError, match="workspace"):
+            pf.pf_lowrank_linear_fwd(x, x, x, workspace=room)
+    with pytest.raises(TypeError):
+        pf.pf_expert_sort(ids, 64, workspace=need)
+    with pytest.raises(pf.PfError) as e:
+        pf.pf_expert_sort(ids, 64, workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == 3

@@ -262,3 +262,12 @@ def test_refusals():
         with pytest.raises(pf.PfError) as e:
             call()
         assert e.value.status == 1
+
+
+def test_a_workspace_that_is_no_whole_buffer_on_the_device_is_refused():
+    q, w, f = normal((50, 4, 64), torch.bfloat16, 1), normal((64,), torch.bfloat16, 3), frequencies(32)
+    need = pf.pf_qk_norm_rope_bwd_workspace(50, 4, 0, 64)
+    for room in (torch.empty(need, dtype=torch.uint8), torch.empty(2 * need, dtype=torch.uint8, device="cuda")[::2],
+                 torch.empty(1, dtype=torch.uint8, device="cuda").expand(need)):
+        with pytest.raises(ValueError, match="workspace"):
+            pf.pf_qk_norm_rope_bwd(q, None, w, None, f, q, None, workspace=room)
