@@ -80,6 +80,16 @@ Stream stream_of(PyObject* o) {
     return {static_cast<cudaStream_t>(p), static_cast<cudaStream_t>(p) == cur};
 }
 
+// An output that the caller has not given, for a call with the argument `stream`.  On a stream other than torch's current one it is
+// recorded, as a workspace is: a caller who drops it at once must not have its memory handed out again while the call still has to write it.
+at::Tensor output(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& like, PyObject* stream) {
+    at::Tensor t = empty(shape, type, like);
+    if (stream == Py_None) return t;
+    const Stream st = stream_of(stream);
+    if (!st.current) c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), c10::cuda::getStreamFromExternal(st.s, like.device().index()));
+    return t;
+}
+
 // The caller's workspace, or a block of torch's caching allocator.  Such a block goes back to the
 // allocator when the wrapper returns, while kernels that use it may still be queued: that is safe on
 // torch's current stream (blocks are reused in stream order) and is made safe on any other stream by
@@ -250,8 +260,8 @@ PyObject* linear_fwd(PyObject* const* a) {
         value_error("bias must be a contiguous [n] tensor of x's dtype");
     const int act = static_cast<int>(integer(a[4]));
     at::Tensor y = optional(a[5], "y"), T = optional(a[6], "T_stash");
-    if (!y.defined()) y = empty({m, n}, x.scalar_type(), x);
-    if (!T.defined() && truth(a[7])) T = empty({m, r}, x.scalar_type(), x);
+    if (!y.defined()) y = output({m, n}, x.scalar_type(), x, a[9]);
+    if (!T.defined() && truth(a[7])) T = output({m, r}, x.scalar_type(), x, a[9]);
     const Stream st = stream_of(a[9]);
     Workspace ws = workspace(a[8], a[8] == Py_None ? pf_lowrank_linear_workspace(m, k, n, r, dt, 0) : 0, x, st);
     auto f = [=, px = ptr(x), pu = ptr(U), pv = ptr(V), pb = ptr(bias), py = ptr(y), pt = ptr(T), ldx = pitch(x, "x"),
@@ -304,9 +314,9 @@ PyObject* linear_bwd(PyObject* const* a) {
     const at::ScalarType gdt = (flags & PF_GRAD_F32) ? at::kFloat : x.scalar_type();
     at::Tensor dX = optional(a[6], "dX"), dU = optional(a[7], "dU"), dV = optional(a[8], "dV");
     if ((flags & PF_GRAD_ACCUMULATE) && (!dU.defined() || !dV.defined())) value_error("accumulate=True needs the dU and dV to add to");
-    if (!dX.defined() && truth(a[5])) dX = empty({m, k}, x.scalar_type(), x);
-    if (!dU.defined()) dU = empty({k, r}, gdt, x);
-    if (!dV.defined()) dV = empty({n, r}, gdt, x);
+    if (!dX.defined() && truth(a[5])) dX = output({m, k}, x.scalar_type(), x, a[12]);
+    if (!dU.defined()) dU = output({k, r}, gdt, x, a[12]);
+    if (!dV.defined()) dV = output({n, r}, gdt, x, a[12]);
     if (dU.scalar_type() != gdt || dV.scalar_type() != gdt)
         value_error("dU and dV must be float32 with grads_f32=True and of x's dtype otherwise");
     const Stream st = stream_of(a[12]);
@@ -333,7 +343,7 @@ PyObject* bias_act_bwd(PyObject* const* a) {
     int64_t m, n;
     rows_cols(dY, "dY", &m, &n);
     at::Tensor db = optional(a[4], "dbias");
-    if (!db.defined() && truth(a[3])) db = empty({n}, dY.scalar_type(), dY);
+    if (!db.defined() && truth(a[3])) db = output({n}, dY.scalar_type(), dY, a[6]);
     const Stream st = stream_of(a[6]);
     Workspace ws = workspace(a[5], db.defined() && a[5] == Py_None ? pf_bias_act_bwd_workspace(m, n) : 0, dY, st);
     auto f = [=, py = ptr(y), pdy = ptr(dY), pdb = ptr(db), ldy = pitch(y, "y"), lddy = pitch(dY, "dY"), wp = ws.p, wb = ws.bytes, s = st.s] {
@@ -367,8 +377,8 @@ PyObject* grouped_fwd(PyObject* const* a) {
     const int64_t G = U.size(0), k = U.size(1), r = U.size(2), n = V.size(1), m = x.size(-2);
     if (V.size(0) != G || V.size(2) != r || x.size(-1) != k) value_error("U must be [G, k, r], V [G, n, r], x [G, m, k] or [m, k]");
     at::Tensor y = optional(a[3], "y"), T = optional(a[4], "T_stash");
-    if (!y.defined()) y = empty({G, m, n}, U.scalar_type(), U);
-    if (!T.defined() && truth(a[5])) T = empty({G, m, r}, U.scalar_type(), U);
+    if (!y.defined()) y = output({G, m, n}, U.scalar_type(), U, a[7]);
+    if (!T.defined() && truth(a[5])) T = output({G, m, r}, U.scalar_type(), U, a[7]);
     const Stream st = stream_of(a[7]);
     const int g = static_cast<int>(G);
     Workspace ws = workspace(a[6], a[6] == Py_None ? pf_lowrank_linear_grouped_workspace(g, m, k, n, r, dt, 0) : 0, U, st);
@@ -394,9 +404,9 @@ PyObject* grouped_bwd(PyObject* const* a) {
     if (U.dim() != 3 || V.dim() != 3 || x.dim() < 2) value_error("U must be [G, k, r], V [G, n, r], x [G, m, k] or [m, k]");
     const int64_t G = U.size(0), k = U.size(1), r = U.size(2), n = V.size(1), m = x.size(-2);
     at::Tensor dX = optional(a[6], "dX"), dU = optional(a[7], "dU"), dV = optional(a[8], "dV");
-    if (!dX.defined() && truth(a[5])) dX = x.dim() == 2 ? empty({m, k}, U.scalar_type(), U) : empty({G, m, k}, U.scalar_type(), U);
-    if (!dU.defined()) dU = empty({G, k, r}, U.scalar_type(), U);
-    if (!dV.defined()) dV = empty({G, n, r}, U.scalar_type(), U);
+    if (!dX.defined() && truth(a[5])) dX = x.dim() == 2 ? output({m, k}, U.scalar_type(), U, a[10]) : output({G, m, k}, U.scalar_type(), U, a[10]);
+    if (!dU.defined()) dU = output({G, k, r}, U.scalar_type(), U, a[10]);
+    if (!dV.defined()) dV = output({G, n, r}, U.scalar_type(), U, a[10]);
     const Stream st = stream_of(a[10]);
     const int g = static_cast<int>(G);
     Workspace ws = workspace(a[9], a[9] == Py_None ? pf_lowrank_linear_grouped_workspace(g, m, k, n, r, dt, 1) : 0, U, st);
@@ -450,8 +460,8 @@ PyObject* conv_fwd(PyObject* const* a) {
     const int dt = dtype_code(x);
     const Conv c = conv_dims(x, U, V, a[3], a[4]);
     at::Tensor y = optional(a[5], "y"), T = optional(a[6], "T_stash");
-    if (!y.defined()) y = empty({c.N, c.Ho, c.Wo, c.O}, x.scalar_type(), x);
-    if (!T.defined() && truth(a[7])) T = empty({c.N, c.Ho, c.Wo, c.R}, x.scalar_type(), x);
+    if (!y.defined()) y = output({c.N, c.Ho, c.Wo, c.O}, x.scalar_type(), x, a[9]);
+    if (!T.defined() && truth(a[7])) T = output({c.N, c.Ho, c.Wo, c.R}, x.scalar_type(), x, a[9]);
     const Stream st = stream_of(a[9]);
     Workspace ws = workspace(a[8], a[8] == Py_None ? conv_workspace(c, dt, 0) : 0, x, st);
     auto f = [=, px = ptr(x), pu = ptr(U), pv = ptr(V), py = ptr(y), pt = ptr(T), wp = ws.p, wb = ws.bytes, s = st.s] {
@@ -476,12 +486,12 @@ PyObject* conv_bwd(PyObject* const* a) {
         value_error("dY must be contiguous [N, Ho, Wo, O]");
     const at::Tensor T = optional(a[6], "T_stash");
     at::Tensor dX = optional(a[8], "dX"), dU = optional(a[9], "dU"), dV = optional(a[10], "dV");
-    if (!dX.defined() && truth(a[7])) dX = empty(x.sizes(), x.scalar_type(), x);
+    if (!dX.defined() && truth(a[7])) dX = output(x.sizes(), x.scalar_type(), x, a[14]);
     const unsigned flags = grad_flags(a[11], a[12]);
     const at::ScalarType gdt = (flags & PF_GRAD_F32) ? at::kFloat : x.scalar_type();
     if ((flags & PF_GRAD_ACCUMULATE) && (!dU.defined() || !dV.defined())) value_error("accumulate=True needs the dU and dV to add to");
-    if (!dU.defined()) dU = empty(U.sizes(), gdt, x);
-    if (!dV.defined()) dV = empty(V.sizes(), gdt, x);
+    if (!dU.defined()) dU = output(U.sizes(), gdt, x, a[14]);
+    if (!dV.defined()) dV = output(V.sizes(), gdt, x, a[14]);
     if (dU.scalar_type() != gdt || dV.scalar_type() != gdt || !dU.is_contiguous() || !dV.is_contiguous())
         value_error("dU and dV must be contiguous, float32 with grads_f32=True and of x's dtype otherwise");
     const Stream st = stream_of(a[14]);
@@ -542,7 +552,7 @@ PyObject* pack(PyObject* const* a) {
     const bool prepare = truth(a[3]);
     TensorList l = tensor_list(a[0], at::Tensor(), "one", prepare);
     const int dt = dtype_code(l.first), count = static_cast<int>(l.ptrs.size());
-    if (!flat.defined()) flat = empty({l.offsets[count]}, l.first.scalar_type(), l.first);
+    if (!flat.defined()) flat = output({l.offsets[count]}, l.first.scalar_type(), l.first, a[2]);
     const Stream st = stream_of(a[2]);
     PyObject* out = Py_BuildValue("(NN)", wrap(flat), offset_list(l.offsets));
     std::vector<at::Tensor> keep = std::move(l.keep);
@@ -659,8 +669,8 @@ PyObject* qk_fwd(PyObject* const* a) {
     const int style = int_of(a[6], "style");
     const double eps = real(a[7]);
     at::Tensor qo = optional(a[8], "q_out"), ko = optional(a[9], "k_out");
-    if (!qo.defined() && r.q.defined()) qo = empty(r.q.sizes(), r.q.scalar_type(), r.q);
-    if (!ko.defined() && r.k.defined()) ko = empty(r.k.sizes(), r.k.scalar_type(), r.k);
+    if (!qo.defined() && r.q.defined()) qo = output(r.q.sizes(), r.q.scalar_type(), r.q, a[10]);
+    if (!ko.defined() && r.k.defined()) ko = output(r.k.sizes(), r.k.scalar_type(), r.k, a[10]);
     const Stream st = stream_of(a[10]);
     auto f = [=, q = heads_of(on, r.q, "q", r.q), k = heads_of(on, r.k, "k", r.k), xq = heads_of(on, qo, "q_out", r.q), xk = heads_of(on, ko, "k_out", r.k),
               wq = ptr(r.wq), wk = ptr(r.wk), pos = static_cast<const int64_t*>(ptr(r.positions)), fr = static_cast<const float*>(ptr(r.inv_freq)),
@@ -685,15 +695,15 @@ PyObject* qk_bwd(PyObject* const* a) {
     const at::Tensor gq = optional(a[8], "dq_out"), gk = optional(a[9], "dk_out");
     if (gq.defined() != r.q.defined() || gk.defined() != r.k.defined()) value_error("dq_out goes with q, dk_out with k");
     at::Tensor dq = optional(a[10], "dq"), dk = optional(a[11], "dk"), dwq = optional(a[13], "dwq"), dwk = optional(a[14], "dwk");
-    if (!dq.defined() && r.q.defined()) dq = empty(r.q.sizes(), any.scalar_type(), any);
-    if (!dk.defined() && r.k.defined()) dk = empty(r.k.sizes(), any.scalar_type(), any);
+    if (!dq.defined() && r.q.defined()) dq = output(r.q.sizes(), any.scalar_type(), any, a[18]);
+    if (!dk.defined() && r.k.defined()) dk = output(r.k.sizes(), any.scalar_type(), any, a[18]);
     const unsigned flags = grad_flags(a[15], a[16]);
     const at::ScalarType wdt = (flags & PF_GRAD_F32) ? at::kFloat : any.scalar_type();
     if (truth(a[12])) {
         if ((flags & PF_GRAD_ACCUMULATE) && ((r.q_heads > 0 && r.wq.defined() && !dwq.defined()) || (r.k_heads > 0 && r.wk.defined() && !dwk.defined())))
             value_error("accumulate=True needs the dwq and dwk to add to");
-        if (!dwq.defined() && r.q_heads > 0 && r.wq.defined()) dwq = empty({r.dim}, wdt, any);
-        if (!dwk.defined() && r.k_heads > 0 && r.wk.defined()) dwk = empty({r.dim}, wdt, any);
+        if (!dwq.defined() && r.q_heads > 0 && r.wq.defined()) dwq = output({r.dim}, wdt, any, a[18]);
+        if (!dwk.defined() && r.k_heads > 0 && r.wk.defined()) dwk = output({r.dim}, wdt, any, a[18]);
     }
     on.check(dwq, "dwq", wdt, 1, true);
     on.check(dwk, "dwk", wdt, 1, true);
@@ -741,10 +751,10 @@ PyObject* expert_sort(PyObject* const* a) {
            "need at least one expert and one choice, and a capacity from 0 on");
     const int64_t rows = pf_expert_rows(tokens, k, experts, capacity);
     at::Tensor slots = optional(a[3], "slots"), sources = optional(a[4], "sources"), counts = optional(a[5], "counts"), offsets = optional(a[6], "offsets");
-    if (!slots.defined()) slots = empty({tokens, k}, at::kInt, ids);
-    if (!sources.defined()) sources = empty({rows}, at::kInt, ids);
-    if (!counts.defined()) counts = empty({experts}, at::kInt, ids);
-    if (!offsets.defined()) offsets = empty({experts + 1}, at::kInt, ids);
+    if (!slots.defined()) slots = output({tokens, k}, at::kInt, ids, a[8]);
+    if (!sources.defined()) sources = output({rows}, at::kInt, ids, a[8]);
+    if (!counts.defined()) counts = output({experts}, at::kInt, ids, a[8]);
+    if (!offsets.defined()) offsets = output({experts + 1}, at::kInt, ids, a[8]);
     on.check(slots, "slots", at::kInt, 2, true);
     on.check(sources, "sources", at::kInt, 1, true);
     on.check(counts, "counts", at::kInt, 1, true);
@@ -788,7 +798,7 @@ PyObject* expert_dispatch_fwd(PyObject* const* a) {
     const Choice c = choice(on, slots, sources, rows);
     const int64_t ldx = matrix(on, x, "x", x.scalar_type(), c.tokens, -1), width = x.size(1);
     at::Tensor xs = optional(a[3], "xs");
-    if (!xs.defined()) xs = empty({rows, width}, x.scalar_type(), x);
+    if (!xs.defined()) xs = output({rows, width}, x.scalar_type(), x, a[4]);
     const int64_t ldxs = matrix(on, xs, "xs", x.scalar_type(), rows, width);
     const Stream st = stream_of(a[4]);
     auto f = [=, px = ptr(x), ps = ints(slots), pr = ints(sources), py = ptr(xs), s = st.s] {
@@ -813,7 +823,7 @@ PyObject* expert_combine_fwd(PyObject* const* a) {
     on.check(weights, "weights", at::kFloat, 2, true);
     expect(!weights.defined() || weights.sizes() == slots.sizes(), "weights must be as slots");
     at::Tensor y = optional(a[3], backward ? "dx" : "y");
-    if (!y.defined()) y = empty({c.tokens, width}, ys.scalar_type(), ys);
+    if (!y.defined()) y = output({c.tokens, width}, ys.scalar_type(), ys, a[4]);
     const int64_t ldy = matrix(on, y, backward ? "dx" : "y", ys.scalar_type(), c.tokens, width);
     const Stream st = stream_of(a[4]);
     auto f = [=, py = ptr(ys), ps = ints(slots), pw = floats(weights), po = ptr(y), s = st.s] {
@@ -841,8 +851,8 @@ PyObject* expert_combine_bwd(PyObject* const* a) {
     expect(weights.sizes() == slots.sizes(), "weights must be as slots");
     const int64_t lddy = matrix(on, dy, "dy", ys.scalar_type(), c.tokens, width);
     at::Tensor dys = optional(a[6], "dys"), dw = optional(a[8], "dweights");
-    if (!dys.defined() && truth(a[5])) dys = empty({rows, width}, ys.scalar_type(), ys);
-    if (!dw.defined() && truth(a[7])) dw = empty(slots.sizes(), at::kFloat, ys);
+    if (!dys.defined() && truth(a[5])) dys = output({rows, width}, ys.scalar_type(), ys, a[9]);
+    if (!dw.defined() && truth(a[7])) dw = output(slots.sizes(), at::kFloat, ys, a[9]);
     const int64_t lddys = matrix(on, dys, "dys", ys.scalar_type(), rows, width);
     on.check(dw, "dweights", at::kFloat, 2, true);
     expect(!dw.defined() || dw.sizes() == slots.sizes(), "dweights must be as slots");

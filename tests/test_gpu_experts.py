@@ -325,3 +325,30 @@ def test_a_workspace_that_is_no_whole_buffer_on_the_device_is_refused():
     with pytest.raises(pf.PfError) as e:
         pf.pf_expert_sort(ids, 64, workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
     assert e.value.status == 3
+
+
+def test_outputs_dropped_at_once_on_another_stream_are_not_handed_out_again():
+    """While the other stream still has to write them: an allocation of the same size on the current stream gets other memory."""
+    ids, x, q, f = choose(3000, 2, 5, 1).cuda(), normal((3000, 64), torch.bfloat16, 1), normal((3000, 4, 64), torch.bfloat16, 2), torch.ones(32, device="cuda")
+    slots, sources, _, _ = pf.pf_expert_sort(ids, 5, capacity=2000)
+    w, side = torch.rand(3000, 2, device="cuda"), torch.cuda.Stream()
+    xs = pf.pf_expert_dispatch_fwd(x, slots, sources)
+    calls = {"sort": lambda: pf.pf_expert_sort(ids, 5, capacity=2000, stream=side), "dispatch": lambda: pf.pf_expert_dispatch_fwd(x, slots, sources, stream=side),
+             "combine": lambda: pf.pf_expert_combine_fwd(xs, slots, w, stream=side),
+             "backward": lambda: pf.pf_expert_combine_bwd(xs, slots, sources, w, x, stream=side), "linear": lambda: pf.pf_lowrank_linear_fwd(x, x[:64], x[:64], stream=side),
+             "norm": lambda: pf.pf_qk_norm_rope_fwd(q, None, None, None, f, stream=side),
+             "norm backward": lambda: pf.pf_qk_norm_rope_bwd(q, None, x[0], None, f, q, None, stream=side)}
+    for name, call in calls.items():
+        call()                                      # (a first launch loads its kernels, which may wait for the device)
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(400_000_000)      # 0.2 s
+        out = call()
+        out = [t for t in (out if isinstance(out, tuple) else (out,)) if t is not None]
+        shapes, places = [(t.shape, t.dtype) for t in out], {t.data_ptr() for t in out}
+        del out
+        again = [torch.empty(s, dtype=d, device="cuda") for s, d in shapes]
+        waiting = not side.query()
+        assert waiting and not places & {t.data_ptr() for t in again}, name
+    torch.cuda.synchronize()
