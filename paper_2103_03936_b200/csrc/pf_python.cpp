@@ -749,6 +749,7 @@ PyObject* expert_sort(PyObject* const* a) {
     const int k = static_cast<int>(ids.size(1));
     expect(experts >= 1 && experts < INT32_MAX && capacity >= 0 && capacity <= INT32_MAX && k >= 1,
            "need at least one expert and one choice, and a capacity from 0 on");
+    if (pf_expert_rows(1, 1, experts, 0) == 0) check(PF_ERR_UNSUPPORTED, "pf_expert_sort");      // (before lists for so many are taken)
     const int64_t rows = pf_expert_rows(tokens, k, experts, capacity);
     at::Tensor slots = optional(a[3], "slots"), sources = optional(a[4], "sources"), counts = optional(a[5], "counts"), offsets = optional(a[6], "offsets");
     if (!slots.defined()) slots = output({tokens, k}, at::kInt, ids, a[8]);

@@ -352,3 +352,13 @@ def test_outputs_dropped_at_once_on_another_stream_are_not_handed_out_again():
         waiting = not side.query()
         assert waiting and not places & {t.data_ptr() for t in again}, name
     torch.cuda.synchronize()
+
+
+def test_experts_that_are_refused_take_no_memory():
+    ids = choose(10, 2, 4, 1).cuda()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    for experts in (2049, 1 << 28):
+        with pytest.raises(pf.PfError) as e:
+            pf.pf_expert_sort(ids, experts)
+        assert e.value.status == 2 and torch.cuda.max_memory_allocated() - before < 1 << 20
