@@ -64,17 +64,22 @@ __device__ __forceinline__ uint64_t turn_per_position(float f) {
     else if (down > 0) turn = (p0 << (64 - down)) | (low >> down);
     return bits >> 31 ? 0 - turn : turn;
 }
-// Cosine and sine.  kExact: to fp32; else the hardware's approximations within half a turn, off by 2^-20.5: 2^-12 of half a step of a bf16 result
-// as large as its pair (with angles in fp64 and sincospif instead
+// Cosine and sine.  kExact: to fp32, the nearest quarter turn taken off as an integer, so that the eighth of a turn that is left has 24 bits of its own.
+// Else the hardware's approximations within half a turn, off by 2^-20.4 (2^-21.2 of their own for angles up to pi, which are off by 2^-21.7 as fp32
+// numbers): 2^-12 of half a step of a bf16 result as large as its pair (with angles in fp64 and sincospif instead
 // the forward of 16384 x 40 heads of 128 took 70 us where it took 66 with these).
 template <bool kExact>
 __device__ __forceinline__ float2 turn_of(int64_t position, uint64_t each) {
-    const float half_turns = static_cast<float>(static_cast<int>((static_cast<uint64_t>(position) * each) >> 32)) * 0x1p-31f;
+    const uint32_t angle = static_cast<uint32_t>((static_cast<uint64_t>(position) * each) >> 32);
     float s, c;
     if constexpr (kExact) {
-        sincospif(half_turns, &s, &c);
+        const uint32_t quarter = (angle + 0x20000000u) >> 30;
+        sincospif(static_cast<float>(static_cast<int>(angle - (quarter << 30))) * 0x1p-31f, &s, &c);
+        const float x = quarter & 1 ? s : c, y = quarter & 1 ? c : s;
+        c = (quarter + 1) & 2 ? -x : x;
+        s = quarter & 2 ? -y : y;
     } else {
-        const float x = half_turns * 3.14159265f;
+        const float x = static_cast<float>(static_cast<int>(angle)) * 0x1p-31f * 3.14159265f;
         s = __sinf(x);
         c = __cosf(x);
     }

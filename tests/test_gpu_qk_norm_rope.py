@@ -271,3 +271,21 @@ def test_a_workspace_that_is_no_whole_buffer_on_the_device_is_refused():
                  torch.empty(1, dtype=torch.uint8, device="cuda").expand(need)):
         with pytest.raises(ValueError, match="workspace"):
             pf.pf_qk_norm_rope_bwd(q, None, w, None, f, q, None, workspace=room)
+
+
+@pytest.mark.parametrize("dim,heads", [(64, 4), (64, 1), (66, 3), (1024, 2)])
+def test_angles_near_quarter_turns(dim, heads):
+    """In fp32 a cosine or sine near zero keeps its digits, as far as an angle in 2^-32 of a turn has them.
+
+    Rows of ones and zeros have r = sqrt(2), to 2^-22 (two units of rsqrt, roundings of 1 / dim and of the mean); sine and cosine to two
+    units and the angle's rounding, the product one more: below 2^-20 of the result.  Of the angle, what is cut off is below 2^-32 of a turn."""
+    half = dim // 2
+    i = torch.arange(half, dtype=torch.float64)
+    f = (torch.pi / 2 * (1 + i % 4) + (i - half / 2) * 1e-6).float().cuda()
+    positions = torch.tensor([0, 1, 3, -5, 1001], device="cuda")
+    x = torch.zeros((5, heads, dim), device="cuda")
+    x[..., :half] = 1
+    out = pf.pf_qk_norm_rope_fwd(x, None, None, None, f, positions=positions, eps=0.0)[0]
+    angle = _ops.angles(positions, f)[:, None]
+    want = 2 ** 0.5 * torch.cat([angle.cos(), angle.sin()], -1).expand_as(out)
+    _ops.close(out, want, 2.0 ** -20 * want.abs() + 2 ** 0.5 * 2 * torch.pi * 2.0 ** -32 * 1.01, "turned")
