@@ -397,8 +397,8 @@ int pf_expert_combine_bwd(const void* ys, int64_t ldys, const int32_t* slots, co
  *   q, q_out [tokens, q_heads, dim]: token t's head h starts at t * ldq + h * sq ELEMENTS; k, k_out likewise (k_heads).  Any
  *            strides under which rows do not overlap (heads inside tokens or tokens inside heads); elements of a row are contiguous.
  *   wq, wk   [dim] in `dtype`, NULL = ones        inv_freq [rot_dim / 2] fp32 (below 2^31)        positions [tokens] int64, NULL = 0, 1, 2, ...
- * Statistics and products are in fp32 and rounded once; an angle is reduced to a part of a turn before it is
- * rounded to fp32, so that far positions (up to 2^40) keep it (sine and cosine then to
+ * Statistics and products are in fp32 and rounded once.  An angle is counted in parts of a turn, those of one position rounded to
+ * 2^-65 of a turn (2^-64 for frequencies above 2^20), so that far positions (up to 2^40: off by 2^-25 of a turn there) keep it; sine and cosine of it to fp32 (to
  * 2^-20 with PF_BF16).  Either of q_heads and k_heads may be 0 (its pointers are ignored then).  rot_dim is even,
  * 0 .. dim.  PF_ERR_UNSUPPORTED: dim > 1024, more than 65536 heads or 2^30 tokens.  One launch, no workspace.
  *

@@ -46,9 +46,11 @@ struct RopeParams {
 };
 
 // Angles are counted in 2^-64 of a turn, modulo a turn: a position times the turn that one position takes is then an integer product, off by at most
-// 2^-64 of a turn for each position (2^-24 at position 2^40), and its upper half is the angle to 2^-32.
+// 2^-65 of a turn for each position (2^-25 at position 2^40), and its upper half is the angle to 2^-32.
 //
-// The turn of one position, f / (2 pi): f's 24 bits times 1 / (2 pi) in 2^-96, moved by f's exponent (f up to 2^31; the whole turns fall off the top).
+// The turn of one position, f / (2 pi): f's 24 bits times 1 / (2 pi) in 2^-96, moved by f's exponent and rounded to nearest (f up to 2^31; the whole
+// turns fall off the top).  The constant is off by less than half of its last bit, 2^23 of the product's last: nothing beside the rounding until f reaches
+// 2^20 (product moved down by 35), a quarter of 2^-64 at 2^31.
 __device__ __forceinline__ uint64_t turn_per_position(float f) {
     constexpr uint32_t k0 = 0x28be60dbu, k1 = 0x9391054au, k2 = 0x7f09d5f4u;      // 2^96 / (2 pi)
     const uint32_t bits = __float_as_uint(f), exponent = (bits >> 23) & 0xffu;
@@ -60,8 +62,8 @@ __device__ __forceinline__ uint64_t turn_per_position(float f) {
     // f = digits 2^(exponent - 150), so that the product is in 2^(exponent - 246) of a turn
     const int down = 182 - static_cast<int>(exponent);
     uint64_t turn = 0;
-    if (down >= 64) turn = down < 128 ? p0 >> (down - 64) : 0;
-    else if (down > 0) turn = (p0 << (64 - down)) | (low >> down);
+    if (down > 64) turn = down < 128 ? ((p0 >> (down - 65)) + 1) >> 1 : 0;
+    else if (down > 0) turn = (down < 64 ? (p0 << (64 - down)) | (low >> down) : p0) + ((low >> (down - 1)) & 1);
     return bits >> 31 ? 0 - turn : turn;
 }
 // Cosine and sine.  kExact: to fp32, the nearest quarter turn taken off as an integer, so that the eighth of a turn that is left has 24 bits of its own.

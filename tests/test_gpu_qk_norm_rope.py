@@ -289,3 +289,20 @@ def test_angles_near_quarter_turns(dim, heads):
     angle = _ops.angles(positions, f)[:, None]
     want = 2 ** 0.5 * torch.cat([angle.cos(), angle.sin()], -1).expand_as(out)
     _ops.close(out, want, 2.0 ** -20 * want.abs() + 2 ** 0.5 * 2 * torch.pi * 2.0 ** -32 * 1.01, "turned")
+
+
+@pytest.mark.parametrize("position", [(1 << 40) - 3, 1 << 40, -(1 << 40) + 12345, 987654321987])
+def test_far_angles_near_quarter_turns(position):
+    """As above at far positions, for frequencies whose angle there is near a quarter turn: a position's part of a turn is rounded to nearest, off by 2^-65."""
+    g = torch.Generator().manual_seed(3)
+    f = torch.cat([torch.rand(200000, generator=g), torch.logspace(-6, 2, 200000)])
+    near = _ops.angles(torch.tensor([position]), f)[0] / (torch.pi / 2)
+    f = f[(near - near.round()).abs().argsort()[:32]].cuda()
+    positions = torch.tensor([position], device="cuda")
+    x = torch.zeros((1, 2, 64), device="cuda")
+    x[..., :32] = 1
+    out = pf.pf_qk_norm_rope_fwd(x, None, None, None, f, positions=positions, eps=0.0)[0]
+    angle = _ops.angles(positions, f)[:, None]
+    want = 2 ** 0.5 * torch.cat([angle.cos(), angle.sin()], -1).expand_as(out)
+    off = 2 ** 0.5 * 2 * torch.pi * (2.0 ** -32 + abs(position) * 2.0 ** -65) * 1.01
+    _ops.close(out, want, 2.0 ** -20 * want.abs() + off, "turned")
