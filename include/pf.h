@@ -396,7 +396,8 @@ int pf_expert_combine_bwd(const void* ys, int64_t ldys, const int32_t* slots, co
  * PF_ROPE_HALVES pairs element i with rot_dim / 2 + i, PF_ROPE_PAIRS element 2 i with 2 i + 1; the other elements stay as they are.
  *   q, q_out [tokens, q_heads, dim]: token t's head h starts at t * ldq + h * sq ELEMENTS; k, k_out likewise (k_heads).  Any
  *            strides under which rows do not overlap (heads inside tokens or tokens inside heads); elements of a row are contiguous.
- *   wq, wk   [dim] in `dtype`, NULL = ones        inv_freq [rot_dim / 2] fp32 (below 2^31)        positions [tokens] int64, NULL = 0, 1, 2, ...
+ *   wq, wk   [dim] in `dtype`, NULL = ones        inv_freq [rot_dim / 2] fp32 (below 2^31; one that is not finite makes its pair NaN)
+ *   positions [tokens] int64, NULL = 0, 1, 2, ...
  * Statistics and products are in fp32 and rounded once.  An angle is counted in parts of a turn, those of one position rounded to
  * 2^-65 of a turn (2^-64 for frequencies above 2^20), so that far positions (up to 2^40: off by 2^-25 of a turn there) keep it; sine and cosine of it to fp32 (to
  * 2^-20 with PF_BF16).  Either of q_heads and k_heads may be 0 (its pointers are ignored then).  rot_dim is even,

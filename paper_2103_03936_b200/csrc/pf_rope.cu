@@ -51,6 +51,8 @@ struct RopeParams {
 // The turn of one position, f / (2 pi): f's 24 bits times 1 / (2 pi) in 2^-96, moved by f's exponent and rounded to nearest (f up to 2^31; the whole
 // turns fall off the top).  The constant is off by less than half of its last bit, 2^23 of the product's last: nothing beside the rounding until f reaches
 // 2^20 (product moved down by 35), a quarter of 2^-64 at 2^31.
+// A frequency that is not finite has kNoTurn, which makes its pair NaN (a finite one of just that turn is moved by 2^-64).
+constexpr uint64_t kNoTurn = 1ull << 63;
 __device__ __forceinline__ uint64_t turn_per_position(float f) {
     constexpr uint32_t k0 = 0x28be60dbu, k1 = 0x9391054au, k2 = 0x7f09d5f4u;      // 2^96 / (2 pi)
     const uint32_t bits = __float_as_uint(f), exponent = (bits >> 23) & 0xffu;
@@ -64,7 +66,8 @@ __device__ __forceinline__ uint64_t turn_per_position(float f) {
     uint64_t turn = 0;
     if (down > 64) turn = down < 128 ? ((p0 >> (down - 65)) + 1) >> 1 : 0;
     else if (down > 0) turn = (down < 64 ? (p0 << (64 - down)) | (low >> down) : p0) + ((low >> (down - 1)) & 1);
-    return bits >> 31 ? 0 - turn : turn;
+    if (turn == kNoTurn) ++turn;
+    return exponent == 255 ? kNoTurn : bits >> 31 ? 0 - turn : turn;
 }
 // Cosine and sine.  kExact: to fp32, the nearest quarter turn taken off as an integer, so that the eighth of a turn that is left has 24 bits of its own.
 // Else the hardware's approximations within half a turn, off by 2^-20.4 (2^-21.2 of their own for angles up to pi, which are off by 2^-21.7 as fp32
@@ -74,6 +77,7 @@ template <bool kExact>
 __device__ __forceinline__ float2 turn_of(int64_t position, uint64_t each) {
     const uint32_t angle = static_cast<uint32_t>((static_cast<uint64_t>(position) * each) >> 32);
     float s, c;
+    if (each == kNoTurn) return make_float2(__int_as_float(0x7fffffff), __int_as_float(0x7fffffff));
     if constexpr (kExact) {
         const uint32_t quarter = (angle + 0x20000000u) >> 30;
         sincospif(static_cast<float>(static_cast<int>(angle - (quarter << 30))) * 0x1p-31f, &s, &c);

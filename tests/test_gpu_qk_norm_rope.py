@@ -306,3 +306,21 @@ def test_far_angles_near_quarter_turns(position):
     want = 2 ** 0.5 * torch.cat([angle.cos(), angle.sin()], -1).expand_as(out)
     off = 2 ** 0.5 * 2 * torch.pi * (2.0 ** -32 + abs(position) * 2.0 ** -65) * 1.01
     _ops.close(out, want, 2.0 ** -20 * want.abs() + off, "turned")
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("dim,heads", [(64, 4), (64, 1), (66, 3), (1024, 2), (256, 2)])
+def test_a_frequency_that_is_not_finite_makes_its_pair_nan(dtype, pairs, dim, heads):
+    """At every position (0 times infinity too), and nothing else of the row."""
+    half = dim // 2
+    x, f = normal((37, heads, dim), dtype, 1), frequencies(half)
+    style = pf.PF_ROPE_PAIRS if pairs else pf.PF_ROPE_HALVES
+    want = pf.pf_qk_norm_rope_fwd(x, None, None, None, f, style=style)[0]
+    bad = [1, half // 2, half - 1]
+    f[bad] = torch.tensor([float("nan"), float("inf"), -float("inf")], device="cuda")
+    got = pf.pf_qk_norm_rope_fwd(x, None, None, None, f, style=style)[0]
+    where = torch.zeros(dim, dtype=torch.bool, device="cuda")
+    for i in bad:
+        where[[2 * i, 2 * i + 1] if pairs else [i, half + i]] = True
+    assert torch.isnan(got[..., where]).all() and torch.equal(got[..., ~where], want[..., ~where])
