@@ -111,10 +111,10 @@ def adamw(p, g, m, v, *, lr, betas, eps, weight_decay, step, grad_scale=1.0):
     return q, slack, m, 2.0 ** -22 * size_m, v, 2.0 ** -22 * size_v
 
 
-def noise(n, seed, tensor):
-    """The 32 random bits of each element of a tensor, as int64."""
-    key = (seed + (tensor + 1) * 0x9E3779B9) & 0xFFFFFFFF
-    x = ((torch.arange(n) ^ key) * 0xA3D95FA7) & 0xFFFFFFFF
+def noise(n, seed, tensor, start=0):
+    """The 32 random bits of each element of a tensor (of n from the place `start` on, all on one side of a multiple of 2^32), as int64."""
+    key = (seed + (tensor + 1) * 0x9E3779B9 + (start >> 32) * 0x9C2F1D35) & 0xFFFFFFFF
+    x = (((torch.arange(n) + (start & 0xFFFFFFFF)) ^ key) * 0xA3D95FA7) & 0xFFFFFFFF
     x = ((x ^ (x >> 15)) * 0xC8B1F265) & 0xFFFFFFFF
     return x ^ (x >> 16)
 

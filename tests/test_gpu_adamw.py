@@ -333,3 +333,55 @@ def test_refusals():
             pf.pf_adamw_step(p, z(), z(), z(), **more)
         assert e.value.status == 1
     assert all((t == 0).all() for t in p)
+
+
+@pytest.mark.parametrize("gdt,masters", [(torch.bfloat16, False), (torch.float32, False), (torch.bfloat16, True)])
+def test_8bit_states_of_a_network(gdt, masters):
+    """Lists of more than 16 blocks for each SM, whose blocks of bf16 parameters take two pieces a thread: whole ones, ragged ones and odd tensors."""
+    sizes = [3_000_064, 2049, 0, 1_900_001, 256 * 16, 300, 200_000]
+    t, checks = state8(sizes, torch.bfloat16, gdt, masters, "own", 0, 11)
+    old = clones(t)
+    pf.pf_adamw_step(**t, **H, seed=21)
+    for check in checks:
+        check()
+    check8(t, old, sizes, masters, H, 21)
+
+
+def test_8bit_states_step_after_step():
+    """Sixty steps from zero, each from what the last one left, bit for bit; gradients of a block from 1 down to 2^-20."""
+    sizes = [256 * 6, 511]
+    t, _ = state8(sizes, torch.float32, torch.float32, False, "own", 0, 12)
+    for name in ("m", "v", "m_scales", "v_scales"):
+        for s in t[name]:
+            s.view(torch.uint8).zero_()
+    g = torch.Generator().manual_seed(12)
+    sizes_of = [2.0 ** (-20 * torch.rand(n, generator=g)) for n in sizes]
+    for step in range(1, 61):
+        for x, s in zip(t["grads"], sizes_of):
+            x.copy_(s * (0.5 + torch.rand(s.shape, generator=g)))
+        old, h = clones(t), H | {"step": step}
+        pf.pf_adamw_step(**t, **h, seed=step)
+        check8(t, old, sizes, False, h, step)
+
+
+def test_8bit_states_of_a_tensor_beyond_32_bits():
+    """The last elements of a tensor of more than 2^32, on either side of that place: codes, scales and random bits by their definition."""
+    border, tail, n = 1 << 32, 512, (1 << 32) + 3000
+    first = border - tail
+    t = {"params": torch.zeros(n, dtype=torch.bfloat16, device="cuda"), "grads": torch.zeros(n, dtype=torch.bfloat16, device="cuda"),
+         "m": torch.zeros(n, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn), "v": torch.zeros(n, dtype=torch.uint8, device="cuda").view(torch.float8_e5m2),
+         "m_scales": torch.zeros(-(-n // 256), device="cuda"), "v_scales": torch.zeros(-(-n // 256), device="cuda")}
+    small, _ = state8([n - first], torch.bfloat16, torch.bfloat16, False, "own", 0, 13)
+    for name in t:
+        (t[name][first // 256:] if "scales" in name else t[name][first:]).copy_(small[name][0])
+    pf.pf_adamw_step(**{k: [x] for k, x in t.items()}, **H, seed=31)
+    m0, v0 = (_ops.decode(small[s][0].cpu(), small[s + "_scales"][0].cpu()) for s in "mv")
+    m, v = _ops.moments32(small["grads"][0].cpu(), m0, v0, H["betas"], H["grad_scale"])
+    bits = torch.cat([_ops.noise(tail, 31, 0, first), _ops.noise(n - border, 31, 0, border)])
+    for s, value, half in (("m", m, bits & 0xFFFF), ("v", v, bits >> 16)):
+        codes, scales = _ops.encode(value, half, s == "m")
+        assert torch.equal(t[s][first:].cpu().view(torch.uint8), codes.view(torch.uint8)), s
+        assert torch.equal(t[s + "_scales"][first // 256:].cpu(), scales), s
+    p, slack = _ops.adamw(small["params"][0].cpu(), small["grads"][0].cpu(), m0, v0, **H)[:2]
+    _ops.close(t["params"][first:].cpu(), p, slack, "params")
+    assert (t["params"][:first] == 0).all()

@@ -362,3 +362,11 @@ def test_experts_that_are_refused_take_no_memory():
         with pytest.raises(pf.PfError) as e:
             pf.pf_expert_sort(ids, experts)
         assert e.value.status == 2 and torch.cuda.max_memory_allocated() - before < 1 << 20
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("width,pitch,shift", [(528, 528, 0), (266, 268, 2), (523, 525, 1)])
+@pytest.mark.parametrize("k,experts,capacity", [(1, 3, 0), (2, 8, 700), (3, 7, 0), (8, 16, 1400)])
+def test_long_rows_of_many_tokens(dtype, width, pitch, shift, k, experts, capacity):
+    """Rows longer than a warp of tokens enough for every warp: the backward of combine by a warp to a token."""
+    test_rows_there_and_back(dtype, width, pitch, shift, 2500, k, experts, capacity)
