@@ -364,7 +364,11 @@ int pf_unpack_factor_grads(const void* flat, int64_t flat_elems, void* const* gr
  *   combine_bwd    dys[slots[t, j]] = weights[t, j] dy[t], other rows zeroed;  dweights[t, j] = <dy[t], ys[slots[t, j]]>, 0 without a row
  *                  (dys or dweights may be NULL: not wanted; weights may not: the gradient of a sum without weights is dispatch_fwd of dy)
  * Sums run over j in order, in fp32, and are rounded once; assignments without a row add nothing, so a token all of whose
- * assignments were dropped gives zeros.  dweights is fp32.  What rows without an assignment hold is never read.  One launch each, no workspace.
+ * assignments were dropped gives zeros.  dweights is fp32.  What rows without an assignment hold is never read.  (PF_BF16 rows with an odd start,
+ * width or pitch are read in aligned 4-byte words, so that two bytes beside a row may be read; they are not used.)  One launch each, no workspace.
+ *
+ * The grouped layers take rows with a capacity: their groups have one shape.  Rows without gaps are for a caller's own products over
+ * offsets[e] .. offsets[e + 1].
  * ------------------------------------------------------------------------------- */
 int64_t pf_expert_rows(int64_t tokens, int k, int experts, int64_t capacity);
 
@@ -401,7 +405,8 @@ int pf_expert_combine_bwd(const void* ys, int64_t ldys, const int32_t* slots, co
  * Statistics and products are in fp32 and rounded once.  An angle is counted in parts of a turn, those of one position rounded to
  * 2^-65 of a turn (2^-64 for frequencies above 2^20), so that far positions (up to 2^40: off by 2^-25 of a turn there) keep it; sine and cosine of it to fp32 (to
  * 2^-20 with PF_BF16).  Either of q_heads and k_heads may be 0 (its pointers are ignored then).  rot_dim is even,
- * 0 .. dim.  PF_ERR_UNSUPPORTED: dim > 1024, more than 65536 heads or 2^30 tokens.  One launch, no workspace.
+ * 0 .. dim.  (Of PF_BF16 rows and weights that do not start and end on 4 bytes, two bytes beside them may be read; they are not used.)
+ * PF_ERR_UNSUPPORTED: dim > 1024, more than 65536 heads or 2^30 tokens.  One launch, no workspace.
  *
  * Backward, for the gradients dq_out and dk_out of the outputs: dq, dk (in `dtype`; always written), and dwq, dwk [dim] (sums over
  * tokens and heads in a fixed order, fp32, rounded once; NULL = not wanted).  The norm's statistics are computed again from q and k.
@@ -444,7 +449,9 @@ int pf_qk_norm_rope_bwd(const void* q, int64_t ldq, int64_t sq, const void* k, i
  *            the state before the first step.  Scales are powers of two that put the largest of a block into [128, 256) (m) and [2^14, 2^15) (v).
  *            A value is rounded up with the probability of what is cut off (16 bits of a hash of seed, i and the element's place in its
  *            tensor; give each step another seed): rounding to nearest would leave v as it is once 1 - beta2 is
- *            below half a step of the format.  Under the format's smallest normal number m becomes 0 and v > 0 that number; what is not
+ *            below half a step of the format.  Under the format's smallest normal number m becomes 0 and v > 0 that number, so that a block's
+ *            smallest elements hardly move: with betas 0.9 and 0.98 and steady gradients of 2^-12 to 2^-13 of the block's largest the mean update is two
+ *            thirds of AdamW's, below that a tenth, below 2^-16 a fiftieth; down to 2^-12 it is AdamW's (1.01 of it).  What is not
  *            finite becomes NaN.  p is stepped with m and v before they are rounded.
  * numels, and the lists of pointers, are host arrays of `count`; tensors with numels 0 are skipped (but count as places).  The
  * arrays of different tensors must not overlap.

@@ -62,10 +62,8 @@ __device__ __forceinline__ int load_cluster(const int* p, uint32_t rank) {
     return v;
 }
 
-// Shared memory: warps x experts counters (which become each warp's next row), then for each expert the block's total, the first row
-// and the whole total.
-// The lanes that have the same value of so many bits, a bit at a time (240 000 assignments to 256 experts on eight blocks: 35 us, with __match_any_sync
-// 40).
+// The lanes whose values have the same lowest `bits` bits, a bit at a time (240 000 assignments to 256 experts on eight blocks: 35 us, with
+// __match_any_sync 40).
 __device__ __forceinline__ unsigned same_value(int value, int bits) {
     unsigned same = 0xffffffffu;
     for (int b = 0; b < bits; ++b) {
@@ -96,6 +94,8 @@ __global__ void __launch_bounds__(kSortThreads) count_kernel(const SortParams p)
     for (int e = threadIdx.x; e < p.experts; e += kSortThreads) p.totals[static_cast<int64_t>(blockIdx.x) * p.experts + e] = sort_smem[e];
 }
 
+// Shared memory: warps x experts counters (which become each warp's next row), then for each expert the block's total, the first row
+// and the whole total.
 template <bool kCluster>
 __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) {
     extern __shared__ int sort_smem[];
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_kernel(const SortParams p) 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const unsigned before = (1u << lane) - 1u;
-    const int bits = 33 - __clz(E);      // (-1 differs from every expert in the highest of them)
+    const int bits = 33 - __clz(E);      // (-1 differs from every expert in the highest of them; `held` has no other value outside)
     constexpr int kHeld = 8;      // assignments of a lane in registers
     int held[kHeld];
     auto hold = [&](int a0) {

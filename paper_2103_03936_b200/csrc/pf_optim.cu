@@ -15,7 +15,9 @@
 // exact, so a value is rounded once.  It is rounded up with the probability of what is cut off (16 random bits from the seed and the
 // element's place): with 1 - beta2 below half a step of the format, rounding to nearest would leave v where it is for
 // ever.  Values below the smallest normal number of the format (2^-14 and 2^-29 of the largest value's binade) become zero in
-// m; in v they become that number, so that a denominator never vanishes.  What is not finite is stored as NaN and leaves its neighbours alone.
+// m; in v they become that number, so that a denominator never vanishes.  Elements whose gradients stay below 2^-12 of their block's largest pay for that
+// with most of their update (steady gradients, 300 steps, beta 0.9 and 0.98: 0.67 of it at 2^-12 to 2^-13, 0.1 below, 0.02 below 2^-16; 1.01 above).
+// What is not finite is stored as NaN and leaves its neighbours alone.
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
