@@ -370,3 +370,24 @@ def test_experts_that_are_refused_take_no_memory():
 def test_long_rows_of_many_tokens(dtype, width, pitch, shift, k, experts, capacity):
     """Rows longer than a warp of tokens enough for every warp: the backward of combine by a warp to a token."""
     test_rows_there_and_back(dtype, width, pitch, shift, 2500, k, experts, capacity)
+
+
+def test_captured_on_a_stream_that_joins_the_capture():
+    """Calls on another stream inside a capture, their lists dropped at once: the replay has other choices and the same results as eager calls."""
+    ids, x = choose(40000, 1, 6, 1).cuda(), normal((40000, 64), torch.bfloat16, 1)
+    side = torch.cuda.Stream()
+
+    def whole(stream):
+        slots, sources, _, _ = pf.pf_expert_sort(ids, 6, capacity=8000, stream=stream)
+        return pf.pf_expert_combine_fwd(pf.pf_expert_dispatch_fwd(x, slots, sources, stream=stream), slots, stream=stream)
+    whole(None)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        out = whole(side)
+        torch.cuda.current_stream().wait_stream(side)
+    for seed in (2, 3):
+        ids.copy_(choose(40000, 1, 6, seed, 0.1))
+        graph.replay()
+        assert torch.equal(out, whole(None))
