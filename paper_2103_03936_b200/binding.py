@@ -10,6 +10,7 @@ defaults.  ``lib()`` is the C library itself through ctypes.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -326,6 +327,8 @@ def pf_adamw_scalars(*, lr, betas=(0.9, 0.999), step, grad_scale=1.0, seed=0):
     (the seed's bits in the last), to be copied into the device tensor that the step reads."""
     if step < 1 or not 0 <= seed < 1 << 32:
         raise ValueError("need a step from 1 on and a seed of 0 .. 2^32 - 1")
+    if not all(0 <= b < 1 for b in betas) or not (math.isfinite(lr) and math.isfinite(grad_scale)):
+        raise ValueError("need betas of 0 .. 1 (without 1), and a finite lr and grad_scale")
     t = torch.tensor([lr, 1 - betas[0] ** step, 1 - betas[1] ** step, grad_scale, 0], dtype=torch.float32)
     t.view(torch.int32)[4] = seed - (1 << 32) if seed >= 1 << 31 else seed
     return t

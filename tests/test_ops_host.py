@@ -168,6 +168,15 @@ def test_scalars_refuse_what_the_step_refuses():
             pf.pf_adamw_scalars(lr=1e-3, **bad)
 
 
+def test_scalars_refuse_what_would_make_every_parameter_infinite_or_nan():
+    """beta = 1 has a correction of zero; lr and grad_scale as the step refuses them."""
+    for bad in (dict(betas=(1.0, 0.98)), dict(betas=(0.9, 1.0)), dict(betas=(-0.1, 0.9)), dict(betas=(0.9, float("nan"))), dict(lr=float("inf")),
+                dict(lr=float("nan")), dict(grad_scale=float("nan")), dict(grad_scale=-float("inf"))):
+        with pytest.raises(ValueError):
+            pf.pf_adamw_scalars(**(dict(lr=1e-3, step=1) | bad))
+    assert pf.pf_adamw_scalars(lr=0.0, betas=(0.0, 0.0), step=3)[:4].tolist() == [0.0, 1.0, 1.0, 1.0]
+
+
 @pytest.mark.parametrize("e4m3", [True, False])
 def test_rounding_of_states_is_fair(e4m3):
     """Mean of what a value is rounded to over the random bits of many places and seeds: the value itself, to the spread of the mean
