@@ -259,11 +259,20 @@ def pf_unpack_factor_grads(flat, grads, *, stream=None):
     return n.unpack(flat, grads, stream)
 
 
+def _fit(ints, longs=()) -> bool:
+    """Whether numbers fit the C types of a size query, which ctypes would cut them to."""
+    return all(abs(v) < 1 << 31 for v in ints) and all(abs(v) < 1 << 63 for v in longs)
+
+
 def pf_expert_rows(tokens, k, experts, capacity=0) -> int:
+    if not _fit((k, experts), (tokens, capacity)):
+        return 0
     return int(lib().pf_expert_rows(tokens, k, experts, capacity))
 
 
 def pf_expert_sort_workspace(tokens, k, experts) -> int:
+    if not _fit((k, experts), (tokens,)):
+        return 0
     return int(lib().pf_expert_sort_workspace(tokens, k, experts))
 
 
@@ -310,6 +319,8 @@ def pf_qk_norm_rope_fwd(q, k, wq, wk, inv_freq, *, positions=None, style=PF_ROPE
 
 
 def pf_qk_norm_rope_bwd_workspace(tokens, q_heads, k_heads, dim) -> int:
+    if not _fit((q_heads, k_heads, dim), (tokens,)):
+        return 0
     return int(lib().pf_qk_norm_rope_bwd_workspace(tokens, q_heads, k_heads, dim))
 
 

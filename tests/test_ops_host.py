@@ -31,6 +31,15 @@ def test_rows_of_refused_sizes():
     assert pf.pf_expert_rows(1 << 29, 2, 4) == 1 << 30 and pf.pf_expert_rows(1, 1, 4, 1 << 28) == 1 << 30
 
 
+def test_queries_of_numbers_beyond_the_c_types():
+    """4 more than 2^32 experts are not 4."""
+    for sizes in ((10, 2, (1 << 32) + 4, 7), (10, (1 << 32) + 2, 4, 7), ((1 << 64) + 10, 2, 4, 0), (10, 2, 4, (1 << 64) + 7)):
+        assert pf.pf_expert_rows(*sizes) == 0, sizes
+    assert pf.pf_expert_sort_workspace(100000, 2, (1 << 32) + 64) == 0 and pf.pf_expert_sort_workspace((1 << 64) + 100000, 2, 64) == 0
+    for sizes in (((1 << 64) + 5, 4, 2, 16), (5, (1 << 32) + 4, 2, 16), (5, 4, 1 << 32, 16), (5, 4, 2, (1 << 32) + 16)):
+        assert pf.pf_qk_norm_rope_bwd_workspace(*sizes) == 0, sizes
+
+
 def test_sort_refuses(L):
     def call(**kw):
         a = dict(ids=P, tokens=10, k=2, experts=4, capacity=0, slots=P, sources=P, counts=P, offsets=P, ws=0, wsb=0, stream=0) | kw
