@@ -222,6 +222,14 @@ __device__ __forceinline__ void bulk_copy(uint32_t to, const void* from, int byt
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
 }
 
+// Of a block that has given up: until its copies have come (fills first .. last - 1 of a ring, one after the other), or once more the time after which it gives up.
+__device__ __noinline__ void wait_for_copies(uint32_t bars, uint32_t first, uint32_t last, uint32_t stages) {
+    const long long t0 = clock64();
+    for (uint32_t f = first; f < last; ++f)
+        while (!tc::mbar_try_wait(bars + 8 * (f % stages), f / stages & 1u))
+            if (clock64() - t0 > tc::kWaitCycleLimit) return;
+}
+
 // Which elements of a row a part has.
 template <typename T>
 struct Part {
@@ -817,7 +825,8 @@ __global__ void __launch_bounds__(kVocabThreads<kMode, kThreads>) vocab_kernel(c
     }
     const RowResult res(all, p.scale);
 
-    const bool ok = *abort_flag == 0;      // (else this part's copies never came)
+    const bool ok = *abort_flag == 0;      // (else this part's copies did not come)
+    if (!ok && t == 0) wait_for_copies(smem_at(sh.bars), 0, static_cast<uint32_t>(chunks), kMaxChunks);
     if (part == 0 && ok) {
         if constexpr (!kDistill) {
             if (t == 0) {
@@ -956,6 +965,12 @@ __global__ void __launch_bounds__(kStreamAll, kStreamBlocks) vocab_stream_kernel
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     auto meet = [] { asm volatile("bar.sync 1, %0;" ::"n"(kStreamThreads) : "memory"); };
+    auto meet_any = [](bool mine) {      // whether any of them says so: the same answer for all
+        uint32_t any;
+        asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n bar.red.or.pred q, 1, %2, p;\n selp.u32 %0, 1, 0, q;\n}"
+                     : "=r"(any) : "r"(static_cast<uint32_t>(mine)), "n"(kStreamThreads) : "memory");
+        return any != 0;
+    };
     auto row_of = [&](int64_t r) { return static_cast<const T*>(p.logits) + r * p.ld; };
     const float c = p.scale * 1.44269504f;
     uint32_t b = 0, b_ph = 0;      // which of the two rows
@@ -967,7 +982,7 @@ __global__ void __launch_bounds__(kStreamAll, kStreamBlocks) vocab_stream_kernel
     if (warp == kWarps) {
         // ---------------------------------------------------------------- chunks
         if (lane == 0) {
-            uint32_t s = 0, ph = 1;
+            uint32_t s = 0, ph = 1, fills = 0;
             bool ok = true;
             for (int64_t r = blockIdx.x; r < p.tokens && ok; r += gridDim.x) {
                 const Part<T> pt(row_of(r), p.vocab, 0, 1);
@@ -978,9 +993,11 @@ __global__ void __launch_bounds__(kStreamAll, kStreamBlocks) vocab_stream_kernel
                     if (!ok) break;
                     bulk_copy(smem_at(data) + s * kStreamChunk * 16, from + static_cast<int64_t>(ck) * kStreamChunk * 16, min(kStreamChunk, pt.count - ck * kStreamChunk) * 16,
                               full0 + 8 * s);
+                    ++fills;
                     if (++s == kStages) { s = 0; ph ^= 1u; }
                 }
             }
+            if (!ok) wait_for_copies(full0, fills > kStages ? fills - kStages : 0, fills, kStages);
         }
         return;
     }
@@ -1043,7 +1060,8 @@ __global__ void __launch_bounds__(kStreamAll, kStreamBlocks) vocab_stream_kernel
         int share = 0, until = per;
         float share_most = -INFINITY;
         for (int ck = 0; ck < chunks && ok; ++ck) {
-            ok = tc::mbar_wait(full0 + 8 * s, ph, abort_flag, p.status);
+            // (a warp gives up as a whole, and no warp but with all others of the block where they meet)
+            ok = __all_sync(0xffffffffu, tc::mbar_wait(full0 + 8 * s, ph, abort_flag, p.status)) != 0;
             if (!ok) break;
             const uint4* const in = reinterpret_cast<const uint4*>(data + s * kStreamChunk * 16) + t;
             const int left = pt.count - ck * kStreamChunk - t;
@@ -1073,6 +1091,7 @@ __global__ void __launch_bounds__(kStreamAll, kStreamBlocks) vocab_stream_kernel
         const bool alone = !top;
         if (alone) {
             if (warp != 0) ok = tc::mbar_wait_warp(smem_at(&sh.stats_empty[b]), b_ph ^ 1u, abort_flag, p.status) && ok;
+            if (!ok) break;
             if (lane == 0) {
                 sh.warp[b][warp] = all;
                 tc::mbar_arrive(smem_at(&sh.stats_full[b]));
@@ -1091,9 +1110,7 @@ __global__ void __launch_bounds__(kStreamAll, kStreamBlocks) vocab_stream_kernel
         }
         if (lane == 0) sh.warp[b][warp] = all;
         ok = tc::mbar_wait_warp(smem_at(&sh.given_full[b]), b_ph, abort_flag, p.status) && ok;
-        meet();
-        ok = ok && *abort_flag == 0;
-        if (!ok) break;
+        if (meet_any(!ok)) break;
         all = block_stats<kWarps>(sh.warp[b], c);
         const RowResult res(all, p.scale);
         if (warp == 0) results(r, res);
