@@ -371,6 +371,12 @@ tc_gated_kernel(const __grid_constant__ CUtensorMap tmT, const __grid_constant__
         }
         if (lane == 0) tma_store_wait_read<0>();
     }
+    // Where a wait has run out, copies and products may be under way, on whose barriers nothing can be built any more: they are given a millisecond (a thousand times what
+    // one takes) before this CTA's memory and its partner's are free.
+    if (*abort_flag) {
+        const long long t0 = clock64();
+        while (clock64() - t0 < kWaitCycleLimit / 2000) {}
+    }
     tc_fence_before();
     __syncthreads();
     cluster_sync_all();          // neither CTA leaves (or frees tensor memory) while the other may still signal it

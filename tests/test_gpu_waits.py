@@ -1,5 +1,5 @@
-"""A wait that runs out ends its kernel with a status: no thread is left behind at a barrier, other blocks' rows are whole, and the device goes on.  (The kernels over
-a vocabulary's rows, compiled with barriers of some blocks that expect more than is copied: tests/device/vocab_waits.cu.)"""
+"""A wait that runs out ends its kernel with a status: no thread is left behind at a barrier, other blocks' rows are whole, and the device goes on.  (Kernels compiled
+with barriers of some blocks that expect more than is copied: tests/device.)"""
 import ctypes
 import os
 import subprocess
@@ -17,12 +17,16 @@ TIMEOUT = 5      # of the status word
 SECONDS = 20     # two limits of two seconds each, and room
 
 
+def built(tmp_path_factory, name):
+    path = str(tmp_path_factory.mktemp("waits") / f"lib{name}.so")
+    include = ["-I", os.path.join(pf_build.ROOT, "include"), "-I", pf_build.CSRC]
+    subprocess.check_call([pf_build.nvcc()] + pf_build.NVCC_FLAGS + include + ["-shared", "-o", path, os.path.join(HERE, "device", name + ".cu")])
+    return ctypes.CDLL(path)
+
+
 @pytest.fixture(scope="module")
 def waits(tmp_path_factory):
-    path = str(tmp_path_factory.mktemp("waits") / "libwaits.so")
-    include = ["-I", os.path.join(pf_build.ROOT, "include"), "-I", pf_build.CSRC]
-    subprocess.check_call([pf_build.nvcc()] + pf_build.NVCC_FLAGS + include + ["-shared", "-o", path, os.path.join(HERE, "device", "vocab_waits.cu")])
-    lib = ctypes.CDLL(path)
+    lib = built(tmp_path_factory, "vocab_waits")
     for name in ("pf_logprobs_fwd", "pf_logprobs_bwd", "pf_distill_fwd", "pf_distill_bwd"):
         getattr(lib, name).argtypes = getattr(pf.lib(), name).argtypes
     torch.zeros(1, device="cuda")
@@ -89,3 +93,36 @@ def test_gradients_and_divergences(waits, rows):
     gives_up(waits, lambda: waits.pf_logprobs_bwd(z.data_ptr(), vocab, ids.data_ptr(), 1.0, ones.data_ptr(), ones.data_ptr(), dz.data_ptr(), vocab, None, None, tokens, vocab,
                                                   pf.PF_BF16, None))
     assert torch.equal(dz[keep], want[keep])
+
+
+@pytest.fixture(scope="module")
+def gates(tmp_path_factory):
+    lib = built(tmp_path_factory, "gated_waits")
+    lib.waits_gated.argtypes = [ctypes.c_void_p] * 4 + [ctypes.c_longlong] * 3
+    return lib
+
+
+@pytest.mark.parametrize("r,backward", [(64, False), (256, False), (320, False), (64, True)])
+def test_gates(gates, r, backward):
+    """Pairs of blocks, of which one's barriers count the copies of both."""
+    lib, m, n = gates, 4096, 2048
+    g = torch.Generator().manual_seed(r)
+    T, V = (torch.randn(s, generator=g).mul_(r ** -0.25).to(torch.bfloat16).cuda() for s in ((2, m, r), (2, n, r)))
+    dY = torch.randn((m, n), generator=g).to(torch.bfloat16).cuda()
+    z = T.double() @ V.double().transpose(1, 2)
+    s = torch.sigmoid(z[0])
+    want = torch.stack((dY.double() * z[1] * (s + z[0] * s * (1 - s)), dY.double() * z[0] * s)) if backward else (z[0] * s * z[1])[None]
+    out = torch.zeros((2 if backward else 1, m, n), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    gives_up(lib, lambda: lib.waits_gated(T.data_ptr(), V.data_ptr(), dY.data_ptr() if backward else None, out.data_ptr(), m, n, r))
+    # tiles of 256 x 128: a run of neighbouring ones to a pair, or every pairs-th
+    pairs, tiles = 74, [(i // 16, i % 16) for i in range(256)]
+    of = [next(p for p in range(pairs) if 256 * p // pairs <= i < 256 * (p + 1) // pairs) if not backward and r <= 256 else i % pairs for i in range(256)]
+    kept = [t for t, p in zip(tiles, of) if 2 * p % 64 != 4]
+    assert len(kept) > 200
+    for a, b in kept:
+        at = (slice(None), slice(256 * a, 256 * a + 256), slice(128 * b, 128 * b + 128))
+        assert float((out[at].double() - want[at]).norm()) <= 1e-2 * float(want[at].norm())
+    x, U = torch.ones((8, 16), dtype=torch.bfloat16, device="cuda"), torch.ones((2, 16, 8), dtype=torch.bfloat16, device="cuda")
+    y = pf.pf_lowrank_linear_gated_fwd(x, U, U)      # (the device goes on: g = u = 128 throughout)
+    assert torch.equal(y, torch.full_like(y, 16384.0)) and pf.pf_last_device_status() == 0
