@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, kNormBlocks<false, kThreads>) norm_k
                 // (a scale below the normal numbers has no inverse: such a block, unless it is all zeros, has the smallest normal number)
                 const bool small = most[u] < 448.f * 0x1p-126f;
                 const float scale = !small ? most[u] * (1.f / 448.f) : most[u] > 0.f ? 0x1p-126f : 0.f;
-                const float inverse = !small ? __fdividef(448.f, most[u]) : 0x1p126f;
+                const float inverse = !small ? __fdividef(448.f * 0x1p-8f, most[u] * 0x1p-8f) : 0x1p126f;      // (its divisors end at 2^126)
                 unsigned codes[kN / 4];
 #pragma unroll
                 for (int i = 0; i < kN / 4; ++i) codes[i] = codes_of(h[u][2 * i], h[u][2 * i + 1], f2(inverse, inverse));

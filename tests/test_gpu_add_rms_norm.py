@@ -264,3 +264,16 @@ def test_arguments_are_checked():
         pf.pf_add_rms_norm_fwd(normal((1, 16392), BF16, 1))
     with pytest.raises(pf.PfError):
         pf.pf_add_rms_norm_bwd(x, w, x, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("block", [0, 32, 128])
+@pytest.mark.parametrize("width", [256, 333])
+def test_codes_of_the_largest_numbers(dtype, block, width):
+    """Weights up to 3e38: blocks whose largest number is above 2^126 have codes up to 448 as any other."""
+    x = normal((6, width), F32, 1).sign().to(dtype)      # (n is 1 or -1)
+    w = torch.tensor([1.0, 1e30, 8e37, 9e37, 1.8e38, 3e38])[torch.arange(width) // 32 % 6].to(dtype).cuda()
+    _, y, y8, scales = pf.pf_add_rms_norm_fwd(x, None, w, block=block)
+    _, _, want, slack = ref.norm(x, None, w, 1e-6)
+    close(y, want, slack, "y")
+    check_codes(y8, scales, want, slack, block)
