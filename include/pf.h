@@ -488,7 +488,8 @@ int pf_adamw_step(void* const* params, float* const* masters, const void* const*
  *            its block (2^-126 at least; 0 for a block of zeros), so codes reach 448; a value is rounded once, to nearest.  scales [tokens, ceil(width / block)],
  *            contiguous.
  * Each of h, y and (y8, scales) may be NULL: not wanted; not all of them.  h may be residual or x (in place), with its pitch.
- * A row that holds an infinity or a NaN gives NaN (codes and scales as well).  Statistics and products are in fp32.
+ * A row whose h holds an infinity or a NaN gives NaN in every element (codes and scales as well; backward: dx).  Statistics and products are in fp32, of rows scaled by a
+ * power of two where their squares would leave its range.
  * PF_ERR_UNSUPPORTED: width > 16384.  One launch, no workspace.
  *
  * Backward, for the gradient dy of y and, NULL = none, dh of h (what reaches the sum by the residual's way):

@@ -10,6 +10,7 @@
 // share a warp or a block.  Blocks stay and walk over rows: the sums for dw are in registers, and a thread's next row is on its way into its own places of shared
 // memory while the present one is computed.
 #include <algorithm>
+#include <type_traits>
 
 #include "pf_internal.h"
 #include "pf_rows.cuh"
@@ -36,7 +37,7 @@ struct NormParams {
     int64_t tokens;
     int width, lanes, warps, rows;     // (lanes of a warp and) warps to a row, rows to a block
     int block, blocks;          // elements to a scale (0: the row), scales of a row
-    float eps;
+    float eps, least;           // (least: see far_off)
 };
 
 __device__ __forceinline__ float max_or_nan(float a, float b) {
@@ -52,20 +53,48 @@ struct Max {
 };
 // What the lanes of a row have, together.  (All threads of the block take part.)  `places`: a number for each warp, another set for each use.
 template <typename Op>
-__device__ __forceinline__ float over_row(float v, float* places, int lanes, int warps, int warp, int row, Op op) {
+__device__ __forceinline__ float in_warp(float v, int lanes, Op op) {
 #pragma unroll
     for (int o = 16; o > 0; o /= 2)
         if (o < lanes) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+template <typename Op>
+__device__ __forceinline__ float of_warps(const float* places, int warps, int row, Op op) {      // a lane's (a warp at most: the same order in every one)
+    const int lane = threadIdx.x & 31;
+    const float v = places[row * warps + (lane < warps ? lane : 0)];
+    return lane < warps ? v : op(0.f, 0.f);
+}
+template <typename Op>
+__device__ __forceinline__ float over_row(float v, float* places, int lanes, int warps, int warp, int row, Op op) {
+    v = in_warp(v, lanes, op);
     if (warps == 1) return v;
     if ((threadIdx.x & 31) == 0) places[warp] = v;
     __syncthreads();
-    const int lane = threadIdx.x & 31;
-    v = places[row * warps + (lane < warps ? lane : 0)];      // (a warp at most: the same order in every one)
-    if (lane >= warps) v = op(0.f, 0.f);
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
-    return v;
+    return in_warp(of_warps(places, warps, row, op), 32, op);
 }
+
+// A row's squares may leave fp32 where the row does not: above 2^64, and (where eps is no more than that) below 2^-63.  Rows whose sum of squares (a warp's part of it) is not
+// between `least` and kMostSquares are multiplied by a power of two and summed again; eps by its square.  *far: whether a row of those that share barriers, or a warp, needs that.
+constexpr float kMostSquares = 0x1p100f, kLeastSquares = 0x1p-60f;
+__device__ __forceinline__ float squares_over_row(float v, float* places, int lanes, int warps, int warp, int row, float least, bool* far) {
+    if (warps == 1) {
+        v = over_row(v, places, lanes, 1, warp, row, Add());
+        *far = __any_sync(0xffffffffu, !(v <= kMostSquares && v >= least));
+        return v;
+    }
+    const int lane = threadIdx.x & 31;
+    v = in_warp(v, 32, Add());
+    if (lane == 0) places[warp] = v;
+    __syncthreads();
+    const float any = places[min(lane, static_cast<int>(blockDim.x >> 5) - 1)];
+    v = of_warps(places, warps, row, Add());
+    *far = __any_sync(0xffffffffu, !(any <= kMostSquares && any >= least));
+    return in_warp(v, 32, Add());
+}
+__device__ __forceinline__ float factor_of(float sum, float least) { return !(sum <= kMostSquares) ? 0x1p-76f : sum < least ? 0x1p90f : 1.f; }
+// ... the second time, in which only rows with an infinity or a NaN have no finite sum: these are NaN throughout.
+__device__ __forceinline__ float finite_or_nan(float sum) { return sum <= 3.4e38f ? sum : __int_as_float(0x7fffffff); }
 
 // Four numbers as e4m3 codes, largest finite one at most.
 __device__ __forceinline__ unsigned codes_of(F2 a, F2 b, F2 inverse) {
@@ -118,6 +147,9 @@ struct NormRing {
     __device__ __forceinline__ void get(int input, int u, F2 (&x)[Unit<T>::kN / 2]) const {
         Unit<T>::get(*reinterpret_cast<const uint4*>(mine + ((now * kInputs + input) * kUnits<T> + u) * apart), x);
     }
+    __device__ __forceinline__ void put(int input, int u, const F2 (&x)[Unit<T>::kN / 2]) {
+        *reinterpret_cast<uint4*>(mine + ((now * kInputs + input) * kUnits<T> + u) * apart) = Unit<T>::pack(x);
+    }
     __device__ __forceinline__ void done() { now = now == kStages - 1 ? 0 : now + 1; }
 };
 // Stages of a ring.  Rows of more than 8192 fp32 elements have no room for two.
@@ -130,7 +162,7 @@ template <typename T, int kPiece, bool kEightBit, int kThreads>
 __global__ void __launch_bounds__(kThreads, kNormBlocks<false, kThreads>) norm_kernel(const NormParams p) {
     constexpr int kN = Unit<T>::kN, kStages = kNormStages<T, kThreads>;
     extern __shared__ __align__(16) unsigned char norm_smem[];
-    __shared__ float places[2][2][kNormMaxWarps];      // sums and largest numbers, of alternate rows
+    __shared__ float places[2][3][kNormMaxWarps];      // sums, largest numbers and sums of rows that are far off, of alternate rows
     const int warp = threadIdx.x >> 5, of_warp = kThreads > 256 ? 32 : p.lanes, lanes = of_warp * p.warps;
     const int row = kThreads > 256 ? 0 : threadIdx.x / static_cast<unsigned>(lanes);
     const NormShare<T> share(threadIdx.x - row * lanes, lanes, p.width);
@@ -181,7 +213,23 @@ __global__ void __launch_bounds__(kThreads, kNormBlocks<false, kThreads>) norm_k
             for (int u = 0; u < kUnits<T>; ++u) weight[u] = load_unit<T, kPiece>(w + share.at[u], share.n[u]);
         }
         const float2 sums = split(sum2);
-        const float rms = rsqrtf(fmaf(over_row(sums.x + sums.y, places[turn][0], of_warp, p.warps, warp, row, Add()), inv_width, p.eps));
+        bool far;
+        float sum = squares_over_row(sums.x + sums.y, places[turn][0], of_warp, p.warps, warp, row, p.least, &far), eps = p.eps;
+        if (far) {
+            const float f = factor_of(sum, p.least);
+            sum2 = f2(0.f, 0.f);
+#pragma unroll
+            for (int u = 0; u < kUnits<T>; ++u)
+#pragma unroll
+                for (int i = 0; i < kN / 2; ++i) {
+                    h[u][i] = mul2(h[u][i], f2(f, f));
+                    sum2 = fma2(h[u][i], h[u][i], sum2);
+                }
+            const float2 again = split(sum2);
+            sum = finite_or_nan(over_row(again.x + again.y, places[turn][2], of_warp, p.warps, warp, row, Add()));
+            eps = eps * f * f;
+        }
+        const float rms = rsqrtf(fmaf(sum, inv_width, eps));
         const F2 scale2 = f2(rms, rms);
 #pragma unroll
         for (int u = 0; u < kUnits<T>; ++u) {
@@ -262,7 +310,7 @@ template <typename T, int kPiece, int kThreads>
 __global__ void __launch_bounds__(kThreads, kNormBlocks<true, kThreads>) norm_bwd_kernel(const NormParams p) {
     constexpr int kN = Unit<T>::kN, kStages = kNormStages<T, kThreads>;
     extern __shared__ __align__(16) unsigned char norm_smem[];      // the ring, then sums for dw of the rows of a block
-    __shared__ float places[2][2][kNormMaxWarps];
+    __shared__ float places[2][4][kNormMaxWarps];      // both sums, and those of rows that are far off, of alternate rows
     const int warp = threadIdx.x >> 5, of_warp = kThreads > 256 ? 32 : p.lanes, lanes = of_warp * p.warps;
     const int row = kThreads > 256 ? 0 : threadIdx.x / static_cast<unsigned>(lanes);
     const NormShare<T> share(threadIdx.x - row * lanes, lanes, p.width);
@@ -294,29 +342,48 @@ __global__ void __launch_bounds__(kThreads, kNormBlocks<true, kThreads>) norm_bw
         ask(t + (kStages - 1) * step);
         ring.wait();
         F2 sum2 = f2(0.f, 0.f), dot2 = f2(0.f, 0.f);      // of h^2 and of h s
+        auto add_up = [&](auto again, float f) {
 #pragma unroll
-        for (int u = 0; u < kUnits<T>; ++u) {
-            F2 h[kN / 2], s[kN / 2];
-            ring.get(0, u, h);
-            ring.get(1, u, s);
-            if (w) {
-                F2 b[kN / 2];
-                Unit<T>::get(load_unit<T, kPiece>(w + share.at[u], share.n[u]), b);
+            for (int u = 0; u < kUnits<T>; ++u) {
+                F2 h[kN / 2], s[kN / 2];
+                ring.get(0, u, h);
+                ring.get(1, u, s);
+                if (w) {
+                    F2 b[kN / 2];
+                    Unit<T>::get(load_unit<T, kPiece>(w + share.at[u], share.n[u]), b);
 #pragma unroll
-                for (int i = 0; i < kN / 2; ++i) s[i] = mul2(s[i], b[i]);
+                    for (int i = 0; i < kN / 2; ++i) s[i] = mul2(s[i], b[i]);
+                }
+                if constexpr (decltype(again)::value) {      // (a power of two: exact, but for what is nothing beside the row's largest)
+#pragma unroll
+                    for (int i = 0; i < kN / 2; ++i) h[i] = mul2(h[i], f2(f, f));
+                    ring.put(0, u, h);
+                }
+#pragma unroll
+                for (int i = 0; i < kN / 2; ++i) {
+                    sum2 = fma2(h[i], h[i], sum2);
+                    dot2 = fma2(h[i], s[i], dot2);
+                }
             }
-#pragma unroll
-            for (int i = 0; i < kN / 2; ++i) {
-                sum2 = fma2(h[i], h[i], sum2);
-                dot2 = fma2(h[i], s[i], dot2);
-            }
-        }
+        };
+        add_up(std::false_type(), 1.f);
         const float2 sums = split(sum2), dots = split(dot2);
-        const float rms = rsqrtf(fmaf(over_row(sums.x + sums.y, places[turn][0], of_warp, p.warps, warp, row, Add()), inv_width, p.eps));
-        // mean(s n), as n = h r
-        const float mean = over_row(dots.x + dots.y, places[turn][1], of_warp, p.warps, warp, row, Add()) * rms * inv_width;
+        bool far;
+        float sum = squares_over_row(sums.x + sums.y, places[turn][0], of_warp, p.warps, warp, row, p.least, &far), f = 1.f;
+        float rms = rsqrtf(fmaf(sum, inv_width, p.eps));
+        float dot = over_row(dots.x + dots.y, places[turn][1], of_warp, p.warps, warp, row, Add());
+        if (far) {      // (h is f h from here on)
+            f = factor_of(sum, p.least);
+            sum2 = dot2 = f2(0.f, 0.f);
+            add_up(std::true_type(), f);
+            const float2 sums2 = split(sum2), dots2 = split(dot2);
+            sum = finite_or_nan(over_row(sums2.x + sums2.y, places[turn][2], of_warp, p.warps, warp, row, Add()));
+            dot = over_row(dots2.x + dots2.y, places[turn][3], of_warp, p.warps, warp, row, Add());
+            rms = rsqrtf(fmaf(sum, inv_width, p.eps * f * f));
+        }
+        const float mean = dot * rms * inv_width;      // of s n, as n = h r
         if (live) {
-            const F2 rr = f2(rms, rms), mm = f2(-mean, -mean);
+            const F2 rr = f2(rms, rms), mm = f2(-mean, -mean), rx = f2(rms * f, rms * f);
             T* const out = static_cast<T*>(p.h) + t * p.ldh;
 #pragma unroll
             for (int u = 0; u < kUnits<T>; ++u) {
@@ -329,7 +396,7 @@ __global__ void __launch_bounds__(kThreads, kNormBlocks<true, kThreads>) norm_bw
                     h[i] = mul2(h[i], rr);
                     dw[u][i] = fma2(s[i], h[i], dw[u][i]);
                     if (w) s[i] = mul2(s[i], b[i]);
-                    h[i] = mul2(rr, fma2(h[i], mm, s[i]));
+                    h[i] = mul2(rx, fma2(h[i], mm, s[i]));
                 }
                 if (p.residual) {
                     ring.get(2, u, b);
@@ -503,6 +570,7 @@ int pf_add_rms_norm_fwd(const void* x, int64_t ldx, const void* residual, int64_
     p.blocks = block ? static_cast<int>(ceil_div(width, block)) : 1;
     p.tokens = tokens; p.width = static_cast<int>(width); p.lanes = pl.lanes; p.warps = pl.warps; p.rows = pl.rows;
     p.eps = static_cast<float>(eps);
+    p.least = p.eps < 1e-18f ? kLeastSquares : 0.f;
     const int piece = piece_of(alignment(x, ldx, dtype) | alignment(residual, ldr, dtype) | alignment(h, ldh, dtype) | alignment(y, ldy, dtype) |
                                alignment(w, 0, dtype) | static_cast<uint64_t>(width) * dtype_size(dtype));
     PF_CUDA(norm_launch(pick_norm(dtype, piece, false, y8 != nullptr, pl.threads), pl, 0, p, static_cast<cudaStream_t>(cuda_stream), pl.groups, &blocks));
@@ -539,6 +607,7 @@ int pf_add_rms_norm_bwd(const void* h, int64_t ldh, const void* w, const void* d
     p.partial = dw ? static_cast<float*>(workspace) : nullptr;
     p.tokens = tokens; p.width = static_cast<int>(width); p.lanes = pl.lanes; p.warps = pl.warps; p.rows = pl.rows;
     p.eps = static_cast<float>(eps);
+    p.least = p.eps < 1e-18f ? kLeastSquares : 0.f;
     const int piece = piece_of(alignment(h, ldh, dtype) | alignment(dh, lddh, dtype) | alignment(dy, lddy, dtype) | alignment(dx, lddx, dtype) |
                                alignment(w, 0, dtype) | static_cast<uint64_t>(width) * dtype_size(dtype));
     const size_t sums = dw && pl.rows > 1 ? sizeof(float) * pl.threads * kLaneElems : 0;      // (16 KB at most)

@@ -277,3 +277,49 @@ def test_codes_of_the_largest_numbers(dtype, block, width):
     _, _, want, slack = ref.norm(x, None, w, 1e-6)
     close(y, want, slack, "y")
     check_codes(y8, scales, want, slack, block)
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("width", [40, 64, 200, 512, 777, 1200, 2500, 4096, 9000, 16384])
+def test_rows_with_an_infinity_are_nan_throughout(dtype, width):
+    """Rows with an infinity or a NaN, given or from the sum: NaN in every element, code and scale, and in every element of their gradient; others are as without them."""
+    x, r, g, w = (normal((7, width), dtype, i) for i in range(4))
+    want = pf.pf_add_rms_norm_fwd(x, r, w[0], block=32)
+    want_dx = pf.pf_add_rms_norm_bwd(want[0], w[0], g, dh=r, need_dw=False)[0]
+    x[1, width // 2], x[3, 0], r[5, width - 1] = float("inf"), float("nan"), float("-inf")
+    x[6, 3] = r[6, 3] = torch.finfo(dtype).max      # (their sum is infinite)
+    bad, good = [1, 3, 5, 6], [0, 2, 4]
+    h, y, y8, scales = pf.pf_add_rms_norm_fwd(x, r, w[0], block=32)
+    y80, scales0 = pf.pf_add_rms_norm_fwd(x, r, w[0], block=0, want_y=False)[2:]
+    dx = pf.pf_add_rms_norm_bwd(h, w[0], g, dh=r, need_dw=False)[0]
+    for t, plain in ((y, want[1]), (y8.float(), want[2].float()), (scales, want[3]), (dx, want_dx)):
+        assert torch.isnan(t[bad]).all() and torch.equal(t[good], plain[good])
+    for t in (y80.float(), scales0):
+        assert torch.isnan(t[bad]).all() and torch.isfinite(t[good]).all()
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("eps", [0.0, 1e-6, 1e-30])
+@pytest.mark.parametrize("layout", ["plain", "odd"])
+@pytest.mark.parametrize("width", [5, 64, 200, 512, 1200, 2500, 4096, 9000, 16384])
+def test_rows_whose_squares_leave_the_range(dtype, eps, layout, width):
+    """Rows of every size that the types hold, beside one another in a block: h^2 is beyond fp32 from 10^19 on and nothing (where eps is, too) from 10^-23 down."""
+    sizes = [1.0, 1e15, 1e19, 1e25, 1e38, 1e-10, 3e17, 1e36] + ([1e-18, 1e-20, 1e-25, 1e-30] if eps < 1e-20 else [])
+    tokens = 2 * len(sizes) + 1
+    size = torch.tensor(sizes + [1.0] + sizes)[:, None].cuda()
+    how = layout_of(layout, width)
+    # (three values of either sign, none of them near nothing: sums are as relatively exact as those of normal rows)
+    pick = lambda seed: torch.tensor([0.5, 1.0, 2.5])[torch.randint(0, 3, (tokens, width), generator=torch.Generator().manual_seed(seed))].cuda()  # noqa: E731
+    x = Rows(tokens, width, dtype, **how).fill((pick(1) * normal((tokens, width), F32, 2).sign() * size).to(dtype))
+    w = (1 + normal((width,), F32, 3, 0.3)).to(dtype)
+    _, y, y8, scales = pf.pf_add_rms_norm_fwd(x.t, None, w, eps=eps, block=128)
+    _, _, want, slack = ref.norm(x.t, None, w, eps)
+    close(y, want, slack, "y")
+    check_codes(y8, scales, want, slack, 128)
+    g = normal((tokens, width), dtype, 4)
+    g = torch.where(size < 1e-4, (g.double() * size).to(dtype), g)      # (gradients of tiny rows are as large as those are small)
+    dx, dw = pf.pf_add_rms_norm_bwd(x.t, w, g, eps=eps, grads_f32=True)
+    want, slack, want_dw, dw_slack = ref.norm_bwd(x.t, w, g, None, eps)
+    # (r below the normal numbers has fewer bits: 2^-149, of what stands beside it; and below 2^-126 bf16's numbers are 2^-133 apart: half a step is 2^-134, not 2^-8 of the value)
+    close(dx, want, slack + 2.0 ** -146 * (1 + g.double().abs()) + (2.0 ** -134 if dtype == BF16 else 0.0), "dx")
+    close(dw, want_dw, dw_slack, "dw")
