@@ -44,7 +44,7 @@ __global__ void __launch_bounds__(256) gate_kernel(const GateParams p) {
                 float value, slope;
                 gate_slope<kAct, true>(g, &value, &slope);
                 const float dy = get(dY + row * p.lddy + c);
-                put(z0 + row * p.ldz + c, dy * u * slope);
+                put(z0 + row * p.ldz + c, dy * slope * u);
                 put(z1 + row * p.ldz + c, dy * value);
             } else {
                 put(y + row * p.ldy + c, gate<kAct>(g) * u);

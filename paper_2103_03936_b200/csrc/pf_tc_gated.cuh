@@ -77,7 +77,7 @@ __device__ __forceinline__ F2 logistic2(F2 x) {
     const F2 e0 = fma2_ftz(d, r0, one), r1 = fma2_ftz(r0, fma2(e0, e0, e0), r0);
     return fma2_ftz(r1, fma2_ftz(d, r1, one), r1);
 }
-// act(g) u of two, approximately.
+// act(g) u of two, approximately: the gate's own value first, as g u may overflow where act(g) is nothing.
 template <int kAct>
 __device__ __forceinline__ F2 gated2(F2 g, F2 u) {
     constexpr float kLog2e = 1.44269504f;
@@ -88,12 +88,12 @@ __device__ __forceinline__ F2 gated2(F2 g, F2 u) {
         return mul2(logistic2(mul2(g, f2(-kLog2e, -kLog2e))), u);
     } else if constexpr (kAct == PF_GATE_GELU) {
         const F2 steep = fma2(mul2(g, g), f2(-kLog2e * kGelu3, -kLog2e * kGelu3), f2(-kLog2e * kGelu1, -kLog2e * kGelu1));
-        return mul2(mul2(g, u), logistic2(mul2(g, steep)));
+        return mul2(mul2(g, logistic2(mul2(g, steep))), u);
     } else {
-        return mul2(mul2(g, u), logistic2(mul2(g, f2(-kLog2e, -kLog2e))));
+        return mul2(mul2(g, logistic2(mul2(g, f2(-kLog2e, -kLog2e)))), u);
     }
 }
-// dY u act'(g) and dY act(g) of two, approximately.  With s = sigmoid(x): 1 - s is off by 2^-24, which beside slopes near 1 is nothing; the sigmoid's own slope
+// dY act'(g) u (in this order) and dY act(g) of two, approximately.  With s = sigmoid(x): 1 - s is off by 2^-24, which beside slopes near 1 is nothing; the sigmoid's own slope
 // takes the form that keeps it.
 template <int kAct>
 __device__ __forceinline__ void gated_grad2(F2 g, F2 u, F2 dy, F2* dg, F2* du) {
@@ -104,7 +104,7 @@ __device__ __forceinline__ void gated_grad2(F2 g, F2 u, F2 dy, F2* dg, F2* du) {
         float a, b, sa, sb;
         gate_slope<kAct, false>(v.x, &a, &sa);
         gate_slope<kAct, false>(v.y, &b, &sb);
-        *dg = mul2(mul2(dy, u), f2(sa, sb));
+        *dg = mul2(mul2(dy, f2(sa, sb)), u);
         *du = mul2(dy, f2(a, b));
     } else if constexpr (kAct == PF_GATE_GELU) {
         const F2 steep = fma2(mul2(g, g), f2(-kLog2e * kGelu3, -kLog2e * kGelu3), f2(-kLog2e * kGelu1, -kLog2e * kGelu1));
@@ -114,12 +114,12 @@ __device__ __forceinline__ void gated_grad2(F2 g, F2 u, F2 dy, F2* dg, F2* du) {
         const F2 near = f2(fminf(fmaxf(v.x, -40.f), 40.f), fminf(fmaxf(v.y, -40.f), 40.f));
         const F2 w = mul2(near, fma2(mul2(near, near), f2(3.f * kGelu3, 3.f * kGelu3), f2(kGelu1, kGelu1)));
         const F2 slope = fma2(mul2(w, s), fma2(s, negated(one), one), s);
-        *dg = mul2(mul2(dy, u), slope);
+        *dg = mul2(mul2(dy, slope), u);
         *du = mul2(dy, h);
     } else {
         const F2 s = logistic2(mul2(g, f2(-kLog2e, -kLog2e))), h = mul2(g, s);
         const F2 slope = fma2(h, fma2(s, negated(one), one), s);
-        *dg = mul2(mul2(dy, u), slope);
+        *dg = mul2(mul2(dy, slope), u);
         *du = mul2(dy, h);
     }
 }

@@ -216,3 +216,27 @@ def test_arguments_are_checked():
         pf.pf_lowrank_linear_gated_fwd(x, U[:1].expand(2, 16, 8), V)
     with pytest.raises(pf.PfError):
         pf.pf_lowrank_linear_gated_fwd(x, U, V, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("n", [16, 130, 1024])
+def test_far_products(dtype, act, n):
+    """Both operands of the product far out: what a gate closes is 0 however large the other side is, also where the two alone would overflow."""
+    g = torch.tensor([-1e20, -1e10, -100.0, -1e25, 1e10, 1e18, 0.0, 2.0]).repeat(-(-n // 8))[:n]
+    u = torch.tensor([1e20, 1e30, 1e38, -1e15, -1e20, 1e20, 1e38, 3e37]).repeat(-(-n // 8))[:n]
+    U, V = torch.zeros(2, 8, 8, dtype=dtype, device="cuda"), torch.zeros(2, n, 8, dtype=dtype, device="cuda")
+    bias = torch.stack((g, u)).to(dtype).cuda()
+    x = normal((3, 8), dtype, 1)
+    y = pf.pf_lowrank_linear_gated_fwd(x, U, V, bias=bias, act=ACTS[act])
+    z, v = bias.double()
+    a = z * torch.sigmoid(1.5957691216057308 * (z + 0.044715 * z ** 3)) if act == "gelu" else ref.act(z, act)
+    want = (a * v).expand(3, n)
+    # (what a gate leaves below 2^-126 may be taken as nothing)
+    close(y, want, 2.0 ** -15 * want.abs() + (2.0 ** -126 * v.abs() * torch.clamp(z.abs(), min=1.0)), "y")
+    got = pf.pf_lowrank_linear_gated_bwd(x, U, V, torch.full_like(y, 1e-30), bias=bias, act=ACTS[act])
+    assert all(torch.isfinite(t).all() for t in got)
+    # gradients that overflow beside u, but not beside a gate that is closed
+    db = pf.pf_lowrank_linear_gated_bwd(x, U, V, torch.full_like(y, 30.0), bias=bias, act=ACTS[act])[3]
+    closed = g <= -100
+    assert torch.isfinite(db[0, closed]).all() and (db[1, closed].abs() <= 1e-30).all()
