@@ -514,9 +514,9 @@ int pf_add_rms_norm_bwd(const void* h, int64_t ldh, const void* w, const void* d
  *   g = (x U0) V0^T + bias0        u = (x U1) V1^T + bias1        y = act(g) * u            y [m, n]
  *   bias [2, n] in `dtype`, contiguous; NULL = none.     act: a pf_gate.
  *   T_stash [2, m, r]: as in the grouped forward; NULL = not written.
- * With PF_BF16 x U is rounded to bf16 before the second product, as everywhere; g and u stay in fp32 up to the one rounding of y.  (bf16 matrices whose width is
- * a multiple of 8 at a pitch, stride or alignment that is not take the grouped layer, which rounds g and u as well; other widths are copied.)
- * Two launches, one more for ragged widths; fp32: both pairs' products side by side and one launch for the gate, for some rows at a time; the smallest fp32 layers and
+ * With PF_BF16 x U is rounded to bf16 before the second product, as everywhere; g and u stay in fp32 up to the one rounding of y.  (k or n above 2^22: g and u
+ * are rounded as well.)
+ * Two launches, one more where matrices at a base, pitch or stride that is not a multiple of 16 bytes are copied (x of k a multiple of 8: two for each 2^23 of its elements); fp32: both pairs' products side by side and one launch for the gate, for some rows at a time; the smallest fp32 layers and
  * other layouts: the launches of the grouped layer and one for the gate.
  *
  * Backward, for dY [m, n]: g and u are computed again,

@@ -2,8 +2,9 @@
 //
 // bf16: T = x U for both pairs in one launch, then both second products with the gate in one (pf_tc_gated.cu); the gate's operands never
 // reach memory; T, and backward dZ, are rounded to bf16, as the tensor cores read them (and as in the factorized layers beside this one).
+// Matrices that TMA cannot read are copied first.
 // fp32: both pairs' products beside one another (pf_tc_f32.cu) for some rows at a time and the gate over their results, which then still are in L2; the smallest
-// ones, and bf16 matrices that TMA cannot read, by the grouped layer (bf16: rounded once more on the way).
+// ones, those that TMA cannot read, and bf16 layers wider than 2^22 by the grouped layer (bf16: g and u are rounded on the way).
 // Backward: the gate's operands again, dZ of both pairs, then the gradients of both.
 #include <algorithm>
 
@@ -70,20 +71,28 @@ int64_t z_pitch(int64_t n) { return (n + 7) / 8 * 8; }
 struct GatedWs {
     size_t off_grouped, off_z, off_sums, total;
 };
+int64_t t_pitch(int64_t r, int dtype) { return dtype == PF_BF16 ? tc::gated_t_pitch(r) : (r + 7) / 8 * 8; }
+bool on_tensor_cores(int64_t k, int64_t n, int64_t r, int dtype) { return dtype == PF_BF16 && tc::gated_fits(k, n, r); }
 GatedWs gated_ws(int64_t m, int64_t k, int64_t n, int64_t r, int dtype, bool bwd) {
     GatedWs w = {};
     const int64_t rows = rows_at_once(m, n);
+    const bool fused = on_tensor_cores(k, n, r, dtype);
     size_t grouped = 0;
-    for (const int64_t part : {rows, m % rows}) grouped = std::max(grouped, pf_lowrank_linear_grouped_workspace(2, part, k, n, r, dtype, 0));
-    size_t off = align_up(static_cast<size_t>(2) * m * ((r + 7) / 8 * 8) * dtype_size(dtype), 256);      // T
+    size_t off = align_up(static_cast<size_t>(2) * m * t_pitch(r, dtype) * dtype_size(dtype), 256);      // T
     w.off_grouped = off;
-    if (dtype == PF_BF16) grouped = std::max(grouped, tc::grouped_workspace(2, m, k, n, r, true));
-    else for (const int64_t part : {rows, m % rows}) grouped = std::max(grouped, tc::f32_gated_workspace(part, k, n, r, false));
-    if (dtype != PF_BF16 && bwd) grouped = std::max(grouped, tc::f32_gated_workspace(m, k, n, r, true));
+    if (fused) {
+        grouped = tc::gated_first_workspace(m, k, n, r);
+    } else {
+        for (const int64_t part : {rows, m % rows}) grouped = std::max(grouped, pf_lowrank_linear_grouped_workspace(2, part, k, n, r, dtype, 0));
+        if (dtype == PF_F32) {
+            for (const int64_t part : {rows, m % rows}) grouped = std::max(grouped, tc::f32_gated_workspace(part, k, n, r, false));
+            if (bwd) grouped = std::max(grouped, tc::f32_gated_workspace(m, k, n, r, true));
+        }
+    }
     if (bwd) grouped = std::max(grouped, pf_lowrank_linear_grouped_workspace(2, m, k, n, r, dtype, 1));
     off += align_up(grouped, 256);
     w.off_z = off;
-    off += align_up(static_cast<size_t>(2) * (bwd ? m : rows) * z_pitch(n) * dtype_size(dtype), 256);
+    if (bwd || !fused) off += align_up(static_cast<size_t>(2) * (bwd ? m : rows) * z_pitch(n) * dtype_size(dtype), 256);
     w.off_sums = off;
     if (bwd) off += align_up(sizeof(float) * act_bwd_chunks(m) * static_cast<size_t>(n), 256);
     w.total = off;
@@ -158,16 +167,14 @@ int pf_lowrank_linear_gated_fwd(const void* x, int64_t ldx, const void* U, int64
     if (rc != PF_OK || m == 0) return rc;
     char* const ws = static_cast<char*>(workspace);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (dtype == PF_BF16) {
+    if (on_tensor_cores(k, n, r, dtype)) {
         const tc::GroupedArgs g = grouped_args(a, T_stash, ldt, st, ws + w.off_grouped, stream);
         tc::GatedArgs ga;
         int handled = 0;
-        rc = tc::gated_first(g, true, &ga, &handled);
-        if (rc != PF_OK) return rc;
-        if (handled) {
-            ga.bias = bias; ga.act = act; ga.y = y; ga.ldy = ldy;
-            return tc::gated(ga, stream);
-        }
+        rc = tc::gated_first(g, true, ws, nullptr, 0, &ga, &handled);
+        if (rc != PF_OK || !handled) return rc != PF_OK ? rc : PF_ERR_CUDA;      // (a driver without tensor maps)
+        ga.bias = bias; ga.act = act; ga.y = y; ga.ldy = ldy;
+        return tc::gated(ga, stream);
     }
     const int64_t rows = rows_at_once(m, n), ldz = z_pitch(n);
     void* const z = ws + w.off_z;
@@ -204,26 +211,20 @@ int pf_lowrank_linear_gated_bwd(const void* x, int64_t ldx, const void* U, int64
     const int64_t ldz = z_pitch(n), sz = m * ldz;
     const void* T = T_stash;
     if (m > 0) {
-        bool done = false;
-        if (dtype == PF_BF16) {
+        if (on_tensor_cores(k, n, r, dtype)) {
             tc::GroupedArgs g = grouped_args(a, T_stash, ldt, st, ws + w.off_grouped, stream);
             g.dY = dY; g.lddy = lddy;
-            if (!T_stash) { g.T = ws; g.ldt = (r + 7) / 8 * 8; g.st = m * g.ldt; }
             tc::GatedArgs ga;
             int handled = 0;
-            rc = tc::gated_first(g, !T_stash, &ga, &handled);
+            rc = tc::gated_first(g, !T_stash, ws, z, ldz, &ga, &handled);      // (a copy of dY in the place of dZ0: the gate reads each tile of it before it writes that)
+            if (rc != PF_OK || !handled) return rc != PF_OK ? rc : PF_ERR_CUDA;
+            ga.bias = bias; ga.act = act; ga.y = z; ga.ldy = ldz; ga.sz = sz;
+            rc = tc::gated(ga, stream);
             if (rc != PF_OK) return rc;
-            if (handled) {
-                ga.bias = bias; ga.act = act; ga.y = z; ga.ldy = ldz; ga.sz = sz;
-                rc = tc::gated(ga, stream);
-                if (rc != PF_OK) return rc;
-                done = true;
-                if (!T_stash) { T = g.T; ldt = g.ldt; st = g.st; }
-            }
-        }
-        if (!done) {
+            T = ga.T; ldt = ga.ldt; st = ga.st;
+        } else {
             const int64_t rows = rows_at_once(m, n);
-            if (!T_stash) { T = ws; ldt = (r + 7) / 8 * 8; st = m * ldt; }
+            if (!T_stash) { T = ws; ldt = t_pitch(r, dtype); st = m * ldt; }
             for (int64_t i = 0; i < m; i += rows) {
                 const int64_t part = std::min(rows, m - i);
                 Matrices some = a;

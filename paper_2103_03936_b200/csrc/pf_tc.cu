@@ -1013,19 +1013,22 @@ struct StagedGroups {
     bool copied = false;
 };
 int stage_groups(const void* p, int64_t ld, int64_t gs, int groups, bool shared, int64_t rows, int64_t cols, char*& scratch,
-                 StagedGroups* out, RepackList* list) {
+                 StagedGroups* out, RepackList* list, bool any = false) {
     *out = StagedGroups{p, ld, gs};
     if (grouped_ok(p, ld, gs)) return 0;
-    if (cols % 8 == 0) return 1;          // the workspace query reserves repack room only for ragged widths
+    if (cols % 8 == 0 && !any) return 1;          // the workspace query reserves repack room only for ragged widths (any: for all)
     const int64_t ldp = row_pitch(cols), n = shared ? 1 : groups;
     list->jobs[list->count++] = RepackJob{p, ld, scratch, ldp, rows, cols, n, gs};
     *out = StagedGroups{scratch, ldp, shared ? 0 : rows * ldp, true};
     scratch += align_up(static_cast<size_t>(n) * rows * ldp * 2, 256);
     return 0;
 }
-size_t groups_room(int groups, int64_t rows, int64_t cols) {
-    return cols % 8 == 0 ? 0 : align_up(static_cast<size_t>(groups) * rows * row_pitch(cols) * 2, 256);
-}
+size_t copy_room(int groups, int64_t rows, int64_t cols) { return align_up(static_cast<size_t>(groups) * rows * row_pitch(cols) * 2, 256); }
+size_t groups_room(int groups, int64_t rows, int64_t cols) { return cols % 8 == 0 ? 0 : copy_room(groups, rows, cols); }
+
+// Rows of x at a time that a gated layer copies: ragged widths at once, others (which lie at a pitch or place that is no multiple of 16 bytes) up to 2^23 elements, so that the
+// room for what hardly ever comes stays small.
+int64_t gated_x_rows(int64_t m, int64_t k) { return k % 8 != 0 ? m : std::min(m, std::max<int64_t>(128, (1LL << 23) / k / 128 * 128)); }
 }  // namespace
 
 size_t grouped_workspace(int groups, int64_t m, int64_t k, int64_t n, int64_t r, bool bwd) {
@@ -1098,44 +1101,74 @@ int linear_grouped_fwd(const GroupedArgs& a, int* handled) {
     return launch_faster(ly, &jy, 1, a.stream);
 }
 
-// What precedes the gate of a gated layer, a grouped layer of two with one x: V, T = x U (need_t: computed, into a.T where that is given; else a.T as
-// the caller has it) and (backward: a.dY) dY as TMA reads them.  a.ws: grouped_workspace(2, ..., true) bytes.
-int gated_first(const GroupedArgs& a, bool need_t, GatedArgs* out, int* handled) {
+int64_t gated_t_pitch(int64_t r) { return row_pitch(r); }
+bool gated_fits(int64_t k, int64_t n, int64_t r) { return k <= (1 << 22) && n <= (1 << 22) && r <= (1 << 22); }
+
+size_t gated_first_workspace(int64_t m, int64_t k, int64_t n, int64_t r) {
+    const int64_t rows = gated_x_rows(m, k);
+    size_t slices = 0;
+    for (const int64_t part : {m, rows, rows > 0 ? m % rows : 0})
+        if (part > 0) slices = std::max(slices, grouped_plan(2, part, k, n, r).p1_bytes);
+    return slices + copy_room(2, k, r) + copy_room(2, n, r) + copy_room(1, rows, k);
+}
+
+// What precedes the gate of a gated layer, a grouped layer of two with one x: V, T = x U (need_t: computed, and kept in a.T where that is given; else a.T as
+// the caller has it) and (backward: a.dY) dY as TMA reads them, copied where they are not.  a.ws: gated_first_workspace bytes; t_room: [2, m, gated_t_pitch(r)], for a T that
+// is nowhere else; dY_room: rows of dY_pitch elements.
+int gated_first(const GroupedArgs& a, bool need_t, void* t_room, void* dY_room, int64_t dY_pitch, GatedArgs* out, int* handled) {
     *handled = 0;
-    if (encode_fn() == nullptr || a.k > (1 << 22) || a.n > (1 << 22) || a.r > (1 << 22)) return PF_OK;
-    const GroupedPlan gp = grouped_plan(2, a.m, a.k, a.n, a.r);
-    char* ws = a.ws;
-    char* Tbuf = ws; ws += gp.t_bytes;
-    const SliceRoom p1{reinterpret_cast<float*>(ws), gp.p1_bytes}; ws += gp.p1_bytes;
-    StagedGroups x, U, V, dY{nullptr, 0, 0}, T{Tbuf, row_pitch(a.r), a.m * row_pitch(a.r)};
-    RepackList repacks;
-    if ((need_t && stage_groups(a.x, a.ldx, 0, 2, true, a.m, a.k, ws, &x, &repacks)) ||
-        (need_t && stage_groups(a.U, a.ldu, a.su, 2, false, a.k, a.r, ws, &U, &repacks)) ||
-        stage_groups(a.V, a.ldv, a.sv, 2, false, a.n, a.r, ws, &V, &repacks) ||
-        (!need_t && stage_groups(a.T, a.ldt, a.st, 2, false, a.m, a.r, ws, &T, &repacks)) ||
-        (a.dY && stage_groups(a.dY, a.lddy, 0, 1, true, a.m, a.n, ws, &dY, &repacks)))
-        return PF_OK;
-    const bool direct = need_t && a.T && grouped_ok(a.T, a.ldt, a.st);
-    if (direct) T = StagedGroups{a.T, a.ldt, a.st};
-    GemmLaunch g1;
-    if (need_t) {
-        const Grouping gt{2, T.gs, false};
-        const int st = gemm_prepare({x.p, x.ld, false, x.gs, false, false}, {U.p, U.ld, true, U.gs, false, false}, a.m, a.r, a.k, const_cast<void*>(T.p), T.ld,
-                                    gp.s1, p1, nullptr, &g1, &gt);
-        if (st == PF_ERR_UNSUPPORTED) return PF_OK;
-        if (st != PF_OK) return st;
-        if (a.T && !direct) { g1.p.C2 = a.T; g1.p.ldc2 = a.ldt; g1.p.c2_gstride = a.st; }
-    }
+    if (encode_fn() == nullptr || !gated_fits(a.k, a.n, a.r)) return PF_OK;
     *handled = 1;
-    *out = GatedArgs{T.p, T.ld, T.gs, V.p, V.ld, V.gs, a.m, a.n, a.r};
-    out->dY = dY.p;
-    out->lddy = dY.ld;
-    int st = repacks.flush(a.stream);
-    if (st != PF_OK || !need_t) return st;
-    if (a.T && !direct) return launch_prepared(g1, a.stream);
-    PairJob jt{x.p, x.ld, false, x.gs, U.p, U.ld, true, U.gs, a.m, a.r, a.k, const_cast<void*>(T.p), T.ld, T.gs, 2};
-    const GemmLaunch* const lt[1] = {&g1};
-    return launch_faster(lt, &jt, 1, a.stream);
+    char* ws = a.ws;
+    StagedGroups U, V;
+    RepackList repacks;
+    if (need_t) stage_groups(a.U, a.ldu, a.su, 2, false, a.k, a.r, ws, &U, &repacks, true);
+    stage_groups(a.V, a.ldv, a.sv, 2, false, a.n, a.r, ws, &V, &repacks, true);
+    const bool direct = a.T && grouped_ok(a.T, a.ldt, a.st);
+    const int64_t ldT = direct ? a.ldt : row_pitch(a.r), sT = direct ? a.st : a.m * row_pitch(a.r);
+    char* const T = static_cast<char*>(direct ? a.T : t_room);
+    if (!need_t && !direct) repacks.jobs[repacks.count++] = RepackJob{a.T, a.ldt, T, ldT, a.m, a.r, 2, a.st};
+    *out = GatedArgs{T, ldT, sT, V.p, V.ld, V.gs, a.m, a.n, a.r};
+    out->dY = a.dY;
+    out->lddy = a.lddy;
+    if (a.dY && !tma_ok(a.dY, a.lddy)) {
+        repacks.jobs[repacks.count++] = RepackJob{a.dY, a.lddy, dY_room, dY_pitch, a.m, a.n};
+        out->dY = dY_room;
+        out->lddy = dY_pitch;
+    }
+    if (!need_t) return repacks.flush(a.stream);
+    const bool x_direct = tma_ok(a.x, a.ldx);
+    const int64_t rows = x_direct ? a.m : gated_x_rows(a.m, a.k), ldx = x_direct ? a.ldx : row_pitch(a.k);
+    char* const x_copy = ws;
+    if (!x_direct) ws += copy_room(1, rows, a.k);
+    for (int64_t i = 0; i < a.m; i += rows) {
+        const int64_t part = std::min(rows, a.m - i);
+        const void* x = a.x;
+        if (!x_direct) {
+            x = x_copy;
+            repacks.jobs[repacks.count++] = RepackJob{static_cast<const char*>(a.x) + 2 * i * a.ldx, a.ldx, x_copy, ldx, part, a.k};
+        }
+        const GroupedPlan gp = grouped_plan(2, part, a.k, a.n, a.r);
+        const SliceRoom slices{reinterpret_cast<float*>(ws), gp.p1_bytes};
+        char* const t = T + 2 * i * ldT;
+        const Grouping gt{2, sT, false};
+        const Operand ox{x, ldx, false, 0, false, false}, ou{U.p, U.ld, true, U.gs, false, false};
+        GemmLaunch g;
+        int st = gemm_prepare(ox, ou, part, a.r, a.k, t, ldT, gp.s1, slices, nullptr, &g, &gt);
+        if (st == PF_ERR_UNSUPPORTED) st = gemm_prepare(ox, ou, part, a.r, a.k, t, ldT, 1, {}, nullptr, &g, &gt);
+        if (st == PF_OK) st = repacks.flush(a.stream);
+        if (st != PF_OK) return st;
+        if (a.T && !direct) {
+            g.p.C2 = static_cast<char*>(a.T) + 2 * i * a.ldt; g.p.ldc2 = a.ldt; g.p.c2_gstride = a.st;
+            st = launch_prepared(g, a.stream);
+        } else {
+            PairJob job{x, ldx, false, 0, U.p, U.ld, true, U.gs, part, a.r, a.k, t, ldT, sT, 2};
+            const GemmLaunch* const list[1] = {&g};
+            st = launch_faster(list, &job, 1, a.stream);
+        }
+        if (st != PF_OK) return st;
+    }
+    return PF_OK;
 }
 
 int linear_grouped_bwd(const GroupedArgs& a, int* handled) {

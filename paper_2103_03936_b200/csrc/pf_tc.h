@@ -142,7 +142,10 @@ struct GatedArgs {
     void* y = nullptr;
     int64_t ldy = 0, sz = 0;
 };
-int gated_first(const GroupedArgs& a, bool need_t, GatedArgs* out, int* handled);      // (pf_tc.cu)
+int64_t gated_t_pitch(int64_t r);      // (these four: pf_tc.cu)
+bool gated_fits(int64_t k, int64_t n, int64_t r);
+size_t gated_first_workspace(int64_t m, int64_t k, int64_t n, int64_t r);
+int gated_first(const GroupedArgs& a, bool need_t, void* t_room, void* dY_room, int64_t dY_pitch, GatedArgs* out, int* handled);
 int gated(const GatedArgs& a, cudaStream_t stream);
 
 size_t linear_extra_workspace(int64_t m, int64_t k, int64_t n, int64_t r, bool bwd);

@@ -26,7 +26,8 @@ class Library:
     def __init__(self, path):
         self.L = ctypes.CDLL(path)
         self.L.host_faults.restype = self.L.host_launches.restype = ctypes.c_char_p
-        for name in ("pf_lowrank_linear_workspace", "pf_lowrank_linear_grouped_workspace", "pf_lowrank_conv_workspace", "pf_bias_act_bwd_workspace"):
+        for name in ("pf_lowrank_linear_workspace", "pf_lowrank_linear_grouped_workspace", "pf_lowrank_linear_gated_workspace", "pf_lowrank_conv_workspace",
+                     "pf_bias_act_bwd_workspace"):
             getattr(self.L, name).restype = ctypes.c_size_t
         self.next = 1 << 40
 
@@ -98,6 +99,25 @@ def grouped(lib, g, m, k, n, r, dtype, *, bwd, stash=True, dX=True, shared=False
                     (mats(m, k, 1 if shared else g) if dX else none) + mats(k, r) + mats(n, r) + sizes, room)
 
 
+def gated(lib, m, k, n, r, dtype, *, bwd, stash=True, dX=True, bias=False, act=0, pads=(0,) * 8, offsets=(0,) * 8):
+    """One gated layer; pads, offsets: elements added to the pitches and places of x, U, V, y or dY, T, dX, dU, dV."""
+    size = 2 if dtype == BF16 else 4
+
+    def mats(i, rows, cols, count):
+        ld = cols + pads[i]
+        step = rows * ld + pads[i]
+        return [(((count - 1) * step + (rows - 1) * ld + cols) * size, offsets[i] * size), ld] + ([step] if count > 1 else [])
+
+    x, U, V, y, T = mats(0, m, k, 1), mats(1, k, r, 2), mats(2, n, r, 2), mats(3, m, n, 1), mats(4, m, r, 2) if stash else [None, 0, 0]
+    b = (2 * n * size, 0) if bias else None
+    sizes = [m, k, n, r, c(dtype)]
+    room = lib.query("pf_lowrank_linear_gated_workspace", m, k, n, r, c(dtype), c(int(bwd)))
+    if not bwd:
+        return lib.call("pf_lowrank_linear_gated_fwd", x + U + V + [b, c(act)] + y + T + sizes, room)
+    return lib.call("pf_lowrank_linear_gated_bwd", x + U + V + [b, c(act)] + y + T + (mats(5, m, k, 1) if dX else [None, 0]) + mats(6, k, r, 2) +
+                    mats(7, n, r, 2) + [b] + sizes, room)
+
+
 def conv(lib, N, H, W, C, R, O, kernel, stride, pad, dtype, *, bwd, stash=True, dX=True, flags=0, room=None):
     size = 2 if dtype == BF16 else 4
     gsize = 4 if flags & GRADS_F32 else size
@@ -122,7 +142,7 @@ def _width(rng, lo, hi):
 
 
 def draw(rng, kind):
-    """Keyword arguments of one call of a kind: linear, linear_f32, grouped, conv or conv_f32, _bwd for the gradients."""
+    """Keyword arguments of one call of a kind: linear, linear_f32, grouped, gated, gated_f32, conv or conv_f32, _bwd for the gradients."""
     bwd = kind.endswith("_bwd")
     dtype = F32 if "f32" in kind else BF16
     kw = dict(bwd=bwd, stash=rng.random() < 0.7)
@@ -138,6 +158,11 @@ def draw(rng, kind):
         return conv, (_log(rng, 1, 256), H, W, C, R, rng.choice((C, 2 * C, _width(rng, 8, 1024))), kernel, stride, pad, dtype), kw
     k, n = _width(rng, 16, 8192), _width(rng, 16, 8192)
     r = min(k, n, _width(rng, 8, 1024) if rng.random() < 0.5 else max(8, k // 4))
+    if kind.startswith("gated"):
+        kw.pop("flags", None)
+        if rng.random() < 0.5:
+            kw["pads"], kw["offsets"] = (tuple(rng.choice((0, 0, 8, 1, 4)) for _ in range(8)) for _ in range(2))
+        return gated, (_log(rng, 1, 20000), k, n, r, dtype), dict(kw, bias=rng.random() < 0.5, act=rng.randrange(4))
     if kind.startswith("grouped"):
         kw.pop("flags", None)
         return grouped, (rng.choice((1, 2, 3, 4, 8, 16)), _log(rng, 1, 8192), k, n, r, F32 if rng.random() < 0.2 else BF16), \
@@ -166,6 +191,10 @@ def fixed(kind):
             yield linear, shape + (BF16,), dict(bwd=True, stash=False, dX=False)
 
 
+    if kind in ("gated", "gated_bwd"):            # x that is copied some rows at a time, alone and beside others
+        for m, k, stash in ((20000, 1024, True), (8193, 1024, False), (9000, 1001, True), (300, 40000, False)):
+            for offsets in ((1, 0, 0, 0, 0, 0, 0, 0), (1,) * 8):
+                yield gated, (m, k, 264, 72, BF16), dict(bwd=kind == "gated_bwd", stash=stash, offsets=offsets)
     if kind == "conv":                            # tall images of few columns, which the boxes of the tensor-core kernels do not reach
         for W, stride in ((4, 4), (3, 3), (1, 3)):
             yield conv, (40, 1400, W, 64, 72, 64, 3, stride, 1, BF16), dict(bwd=False)

@@ -22,7 +22,14 @@
 namespace {
 struct Range {
     uint64_t base, bytes;
+    uint64_t row = 0, pitch = 0;      // bytes of its rows, and from one to the next, where that is known
 };
+// Rows of one pitch that lie side by side share no bytes.
+bool beside(const Range& a, const Range& b) {
+    if (a.pitch == 0 || a.pitch != b.pitch) return false;
+    const uint64_t d = (b.base % a.pitch + a.pitch - a.base % a.pitch) % a.pitch;
+    return d >= a.row && d + b.row <= a.pitch;
+}
 std::vector<Range> regions, written;      // `written`: what the products of the launch in hand write
 // What may still be being written when that launch starts: by the launch before, and, behind one that lets its successor start
 // without having waited itself, by what that one ran beside.
@@ -45,11 +52,12 @@ void inside(const std::string& what, uint64_t base, uint64_t bytes) {
     faults += what + ": " + std::to_string(bytes) + " bytes, " + (past ? std::to_string(past) + " of them past the end of their buffer\n" : "in no buffer\n");
 }
 // ... and what the products of one launch write there may not overlap.
-void writes(const std::string& what, uint64_t base, uint64_t bytes) {
+void writes(const std::string& what, uint64_t base, uint64_t bytes, uint64_t row = 0, uint64_t pitch = 0) {
     inside(what, base, bytes);
+    const Range r{base, bytes, row, pitch};
     for (const Range& w : written)
-        if (base < w.base + w.bytes && w.base < base + bytes) faults += what + ": overlaps what another product of the launch writes\n";
-    written.push_back(Range{base, bytes});
+        if (base < w.base + w.bytes && w.base < base + bytes && !beside(w, r)) faults += what + ": overlaps what another product of the launch writes\n";
+    written.push_back(r);
 }
 uint64_t matrix(int64_t rows, int64_t cols, int64_t ld, int64_t size) { return rows > 0 ? static_cast<uint64_t>(((rows - 1) * ld + cols) * size) : 0; }
 
@@ -66,7 +74,7 @@ void check(const pf::tc::GemmParams& p) {
 void check(const pf::tc::F32Params& p) {
     if (p.splits > 1) writes("slices of an fp32 product", address(p.partial), static_cast<uint64_t>(p.tiles_x) * p.tiles_y * p.splits * 128 * p.bn * 4);
     const bool whole = p.mode == 0 || p.mode == 2;      // (else the pixels of the images)
-    if (whole || p.splits <= 1) writes("result of an fp32 product", address(p.C), matrix(whole ? p.M : static_cast<int64_t>(p.cv_N) * p.out_h * p.out_w, p.N, p.ldc, 4));
+    if (whole || p.splits <= 1) writes("result of an fp32 product", address(p.C), matrix(whole ? p.M : static_cast<int64_t>(p.cv_N) * p.out_h * p.out_w, p.N, p.ldc, 4), 4ull * p.N, 4ull * p.ldc);
     if (p.C2) writes("second copy of an fp32 result", address(p.C2), matrix(p.M, p.N, p.ldc2, 4));
 }
 constexpr uint64_t kSlice = 128 * 64 * 4;
@@ -144,7 +152,8 @@ void launched(const void* kernel, unsigned blocks, void** args) {
     } else if (is("repack_multi_kernel")) {
         const pf::RepackBatchArgs& a = arg<pf::RepackBatchArgs>(args, 0);
         for (int j = 0; j < a.count; ++j)
-            writes("copy", address(a.dst[j]), matrix((a.item_end[j] - (j > 0 ? a.item_end[j - 1] : 0u)) / a.pieces_per_row[j], a.pieces_per_row[j] * 8, a.ld_dst[j], 2));
+            writes("copy", address(a.dst[j]), matrix((a.item_end[j] - (j > 0 ? a.item_end[j - 1] : 0u)) / a.pieces_per_row[j], a.pieces_per_row[j] * 8, a.ld_dst[j], 2),
+                   a.pieces_per_row[j] * 16ull, a.ld_dst[j] * 2ull);
     } else if (is("tc_chain_kernel") || is("tc_chain_pipe_kernel")) {
         const pf::tc::ChainParams& p = arg<pf::tc::ChainParams>(args, 5);
         if (p.tiles_per_split > 0) stored("output of the fused kernel", arg<CUtensorMap>(args, 3));
@@ -152,11 +161,14 @@ void launched(const void* kernel, unsigned blocks, void** args) {
         late = is("Li3E") && p.group_flags[1];
     } else if (is("tc_f32_kernel")) {
         const pf::tc::F32Launch& l = arg<pf::tc::F32Launch>(args, 0);
-        for (int i = 0; i < 3; ++i)
+        for (int i = 0; i < pf::tc::kF32Products; ++i)
             if (i == 0 || l.end[i] > l.end[i - 1]) {
                 check(l.p[i]);
                 early(l.p[i].early, l.ta[i], l.tb[i]);
             }
+    } else if (is("tc_gated_kernel")) {      // (results that TMA cannot store have no map: T's stands in its place)
+        const MapNote& n = reinterpret_cast<const MapNote&>(arg<CUtensorMap>(args, 2));
+        writes("result of a gate", n.base, n.bytes);
     } else if (is("tc_conv_dt_dv_kernel")) {
         const pf::tc::DtDvParams& p = arg<pf::tc::DtDvParams>(args, 3);
         check(p, blocks);

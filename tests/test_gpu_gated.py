@@ -240,3 +240,42 @@ def test_far_products(dtype, act, n):
     db = pf.pf_lowrank_linear_gated_bwd(x, U, V, torch.full_like(y, 30.0), bias=bias, act=ACTS[act])[3]
     closed = g <= -100
     assert torch.isfinite(db[0, closed]).all() and (db[1, closed].abs() <= 1e-30).all()
+
+
+@pytest.mark.parametrize("act", list(ACTS))
+@pytest.mark.parametrize("odd", ["x", "U", "V", "T", "y", "x U V T y"])
+@pytest.mark.parametrize("m,k,n,r", [(158, 728, 224, 112), (97, 8, 288, 8), (2000, 16, 1736, 40), (9000, 1000, 72, 16)])
+def test_bf16_matrices_at_odd_places(act, odd, m, k, n, r):
+    """Matrices of whole 16-byte rows that do not lie on 16 bytes: what g and u are is rounded no more than where they do, so that the results are the same, and
+    gradients are as near (g of max(0, .) on the right side of zero)."""
+    def place(t, name, pair=False):
+        if name not in odd.split():
+            return t
+        rows, cols = t.shape[-2:]
+        gs, ld = rows * (cols + 3) + 5, cols + 3
+        out = torch.zeros((2 if pair else 1) * gs + 64, dtype=BF16, device="cuda")
+        return (out.as_strided((2, rows, cols), (gs, ld, 1), 1) if pair else out.as_strided((rows, cols), (ld, 1), 1)).copy_(t)
+    x, U, V = normal((m, k), BF16, 1), normal((2, k, r), BF16, 2, k ** -0.5), normal((2, n, r), BF16, 3, 1.5 * r ** -0.5)
+    b, dY = normal((2, n), BF16, 4, 0.5), normal((m, n), BF16, 5)
+    y, T = pf.pf_lowrank_linear_gated_fwd(x, U, V, bias=b, act=ACTS[act], want_stash=True)
+    x_, U_, V_, dY_ = place(x, "x"), place(U, "U", True), place(V, "V", True), place(dY, "y")
+    T_, y_ = place(torch.zeros_like(T), "T", True), place(torch.zeros_like(y), "y")
+    ws = Scratch(pf.pf_lowrank_linear_gated_workspace(m, k, n, r, pf.PF_BF16, False))
+    pf.pf_lowrank_linear_gated_fwd(x_, U_, V_, bias=b, act=ACTS[act], y=y_, T_stash=T_, workspace=ws.t)
+    ws.check()
+    exact_T = x.double() @ U.double()
+    for t in (T, T_):
+        close(t, exact_T, 2.0 ** -18 * (x.double().abs() @ U.double().abs()), "T")
+    want, slack = ref.gated(T_, V, b, act)
+    close(y_, want, slack, "y")
+    for stash in (T_, None):
+        ws = Scratch(pf.pf_lowrank_linear_gated_workspace(m, k, n, r, pf.PF_BF16, True))
+        dX, dU, dV, db = pf.pf_lowrank_linear_gated_bwd(x_, U_, V_, dY_, bias=b, act=ACTS[act], T_stash=stash, workspace=ws.t)
+        ws.check()
+        z = (T_.double() @ V.double().transpose(1, 2) + b.double()[:, None]).requires_grad_()
+        dZ = torch.autograd.grad(ref.act(z[0], act) * z[1], z, dY.double())[0]
+        G = dZ @ V.double()
+        near(dX, (G @ U.double().transpose(1, 2)).sum(0), GRAD[BF16], "dX")
+        near(dU, x.double().T @ G, GRAD[BF16], "dU")
+        near(dV, dZ.transpose(1, 2) @ T_.double(), GRAD[BF16], "dV")
+        near(db, dZ.sum(1), GRAD[BF16], "dbias")

@@ -53,3 +53,9 @@ assert named("tc_conv_res_kernel") + named("tc_chain") == 1 and named("repack") 
 """
     done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
     assert done.returncode == 0, done.stderr
+
+
+@pytest.mark.parametrize("kind", ["gated", "gated_bwd", "gated_f32", "gated_f32_bwd"])
+def test_gated_layers_reach_nothing_outside_their_buffers(host_library, kind):
+    """The same for gated layers, with matrices at any place and pitch."""
+    test_nothing_reaches_outside_the_buffers_of_a_call(host_library, kind)
