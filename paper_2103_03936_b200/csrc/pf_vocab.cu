@@ -32,8 +32,9 @@ constexpr int kOwners = 256;           // shares that are gone through again at 
 constexpr int64_t kPartBytes = 65536, kPartBytesMost = 200 << 10, kPartBytesLeast = 8192;
 constexpr int kDeep = 4, kMaxChunks = 16;      // pieces of a thread in a chunk of the row, one bulk copy; chunks (13 of 256 threads in 200 KB)
 // A term e^d d of a logit of -infinity, or of one so far below the largest that d is, has to be 0 and not NaN.  Beside a largest logit between -kFar and kFar, logits below
-// -2^100 are taken as that, which leaves d finite at every scale (4e36 at most); elsewhere exponents below kLeast are taken as that (a few instructions more).
-constexpr float kFar = 1e30f, kLowest = -0x1p100f, kLeast = -1e5f;
+// -2^100 are taken as that, which leaves d finite at every scale (distances of kFarthest at most).  Elsewhere, and where the gradient times that distance is not finite, exponents
+// below kLeast, whose powers are 0, are taken as that (a few instructions more).
+constexpr float kFar = 1e30f, kLowest = -0x1p100f, kFarthest = 2.3e30f, kLeast = -200.f;
 
 struct VocabParams {
     const void* logits;
@@ -883,7 +884,7 @@ __global__ void __launch_bounds__(kVocabThreads<kMode, kThreads>) vocab_kernel(c
                 store_piece(pieces + static_cast<int64_t>(i) * kN, whole, Logits<T>::pack(x));
             }
         };
-        if (kDistill || fabsf(res.base) <= kFar) write(std::false_type());
+        if (kDistill || (fabsf(res.base) <= kFar && fabsf(g.b) * (kFarthest * c) <= 1e38f)) write(std::false_type());
         else write(std::true_type());
         if (has_extra) Logits<T>::put(out + extra, g.one(beside));
         __syncthreads();      // the given tokens' elements, written anew behind the others
