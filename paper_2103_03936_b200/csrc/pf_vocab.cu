@@ -354,9 +354,8 @@ struct RowResult {
         entropy = nothing ? 0.f : log_s - 0.69314718f * (all.w / all.s);
         scale = scale_;
     }
-    __device__ __forceinline__ float logprob(float z) const {
-        const float d = z - base;
-        return nothing ? -INFINITY : (d >= -3.4e38f ? scale * d : fmaf(scale, z, -scale * base)) - log_s;      // (two ends of the range are further apart than it is long)
+    __device__ __forceinline__ float logprob(float z) const {      // (by halves: the two ends of the range are further apart than it is long)
+        return nothing ? -INFINITY : 2.f * (scale * (0.5f * z - 0.5f * base)) - log_s;
     }
     __device__ __forceinline__ float lse() const { return nothing ? -INFINITY : fmaf(scale, base, log_s); }
 };
