@@ -390,9 +390,10 @@ __device__ __forceinline__ void store_piece(T* to, bool whole, uint4 v) {
 }
 
 // The largest elements of a row or part, by kThreads threads.  The largest of each of kKeys shares of the pieces are known (keys: order_of, of bf16 logits its upper half;
-// 0: an empty share); the k-th of those is a bound that at least k elements reach, found bit by bit by each warp for itself; few more do, all of them in shares
-// that reach it, which are gone through again; they are ranked against one another.  Where too many are equal to the bound, those above it and the first k that equal it
-// are; where that is not enough (too many above it, or NaN among the largest) they are found one after the other.
+// 0: an empty share); the k-th of those is a bound that at least k elements reach, found bit by bit by each warp for itself.  With k up to three quarters of the shares few more
+// do (with more the bound is near the least of their largest, and 0 where there are not as many); all are in shares that reach it, which are gone through again, and are ranked
+// against one another.  Where too many are equal to the bound, those above it and the first k that equal it are; where that is not enough (too many above it, or NaN among the
+// largest) they are found one after the other.
 //   piece(i): piece i of `pieces`; element e of it is the row's place0 + i kN + e.   piece_of(share, j): the share's j-th piece, j < each (`pieces` or more: none).
 //   beside(j), j < 16: an element outside the pieces, its place in *place, or false.
 //   use: 0 and 1 in turn, whose counters are zero.  meet(): a barrier of the kThreads threads.  rank_of(key, rank) is called once for each of the k largest, by some thread.
@@ -1146,7 +1147,10 @@ struct VocabPlan {
 };
 // Forward, rows of more than 64 KB of which every SM has two or more stream (2048 x 131072: 92 us; as parts 147).  Others: parts of at most 64 KB; more of them, of 8 KB at
 // least, while rows are too few for the SMs.  Short rows have small blocks, of which an SM holds more.  (All four operators add up rows of parts in the same order.)
-bool vocab_plan(int64_t tokens, int64_t vocab, int dtype, VocabPlan* pl) {
+// Short rows of which many alternatives are wanted have blocks of more threads than that, for more shares (2048 rows of 4000, 128 alternatives: 128 threads, one after the
+// other, 898 us, 256 threads 45; 1000, 64: 32 threads 196, 128 threads 17; but 4000, 65: 22.6 and 31.9), unless all of a row can be ranked or there are fewer pieces than alternatives
+// anyway (1000, 128, one after the other: 32 threads 378, 256 threads 508).
+bool vocab_plan(int64_t tokens, int64_t vocab, int dtype, int top, VocabPlan* pl) {
     const int64_t bytes = vocab * static_cast<int64_t>(dtype_size(dtype));
     pl->stream = bytes > kPartBytes && tokens >= 2 * num_sms();
     pl->parts = 1;
@@ -1154,7 +1158,8 @@ bool vocab_plan(int64_t tokens, int64_t vocab, int dtype, VocabPlan* pl) {
     while (pl->parts < kMaxParts && tokens * pl->parts < num_sms() && bytes / (2 * pl->parts) >= kPartBytesLeast) pl->parts *= 2;
     const int64_t part = ceil_div(ceil_div(bytes, 16), pl->parts) * 16;
     if (part > kPartBytesMost) return false;
-    pl->threads = part <= 2048 ? 32 : part <= 16384 && pl->parts == 1 ? 128 : 256;
+    auto enough = [&](int threads) { return vocab <= kCollected || 4 * top <= 3 * threads || bytes / 16 < top; };
+    pl->threads = part <= 2048 && enough(32) ? 32 : part <= 16384 && pl->parts == 1 && enough(128) ? 128 : 256;
     pl->part = static_cast<size_t>(part);
     return true;
 }
@@ -1181,7 +1186,7 @@ int vocab_launch(const VocabParams& p, const VocabPlan& pl, cudaStream_t stream)
 template <int kMode>
 int vocab_run(VocabParams& p, int64_t tokens, int64_t vocab, int dtype, double scale, cudaStream_t stream) {
     VocabPlan pl;
-    if (!vocab_plan(tokens, vocab, dtype, &pl)) return PF_ERR_UNSUPPORTED;
+    if (!vocab_plan(tokens, vocab, dtype, p.top, &pl)) return PF_ERR_UNSUPPORTED;
     p.tokens = tokens;
     p.vocab = static_cast<int>(vocab);
     p.parts = pl.parts;
