@@ -733,7 +733,7 @@ __device__ __forceinline__ void f32_tile(const CUtensorMap& tmA, const CUtensorM
     if (*repair) f32_repair<BN, kMode>(p, bx, by, bz);
 }
 
-// Up to three independent products in one launch, blocks [end[i - 1], end[i]) working on product i; kConv compiles the
+// Up to kF32Products independent products in one launch, blocks [end[i - 1], end[i]) working on product i; kConv compiles the
 // convolution's addressing modes in (a translation unit of its own, as for the bf16 kernels).
 template <int kMode>
 __device__ __forceinline__ void f32_any(const CUtensorMap& ta, const CUtensorMap& tb, const F32Params& p, int idx) {

@@ -9,8 +9,8 @@
 //                         gradient; the parts of a row are a cluster, whose blocks read one another's M, S and W.  64 KB leave room for three blocks on an SM, one of which
 //                         loads while another computes or stores.
 //   vocab_stream_kernel   forward of many long rows: three blocks stay on each SM and walk over rows, chunks of which (16 KB) come through a ring, asked for across rows' ends.
-// 2048 x 131072 bf16: log probabilities and entropy 92 us (5.8 TB/s), with 20 alternatives 123, gradient 252 (4.3 TB/s); 4096 x 32001: 59 us (4.4 TB/s), with 8 79,
-// gradient 113 (4.6 TB/s); divergence from 64 entries, 4096 x 32768: 66 us, gradient 115.
+// 2048 x 131072 bf16: log probabilities and entropy 93 us (5.8 TB/s), with 20 alternatives 125, gradient 241 (4.5 TB/s); 4096 x 32001: 60 us (4.4 TB/s), with 8 79,
+// gradient 99 (5.3 TB/s); divergence from 64 entries, 4096 x 32768: 66 us, gradient 113.
 // A thread takes the largest of four pieces of 16 bytes before their powers.
 #include <algorithm>
 #include <cmath>
